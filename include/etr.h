@@ -417,6 +417,99 @@ etr_status etr_read_status(const etr_stats* stats_dev, etr_stats* stats_host, vo
  * error_word (etr_layer_forward does) before the next ordinary use of `stats`. */
 etr_status etr_selftest_bounded_wait(etr_stats* stats, int64_t limit_cycles, void* stream);
 
+/* ---- tokens sorted by a choice of experts that the caller made ----------------------------------- */
+
+/* For a router of the caller's own: any choice of k experts per token, with any weights, takes the tokens to their experts
+ * and the experts' outputs back, with the gradients of both.  An expert id outside [0, E) means no expert (padding): the
+ * pair gets no row, adds nothing to Y, and its weight's gradient is 0; its weight is not read.  A token may name an expert
+ * twice (two rows).
+ *
+ * Rows: expert e's pairs, in ascending (token, choice) order, take counts[e] rows from offsets[e] on.
+ *   capacity = 0: nothing is dropped; the experts' rows follow one another, each expert's start at a multiple of `align`
+ *                 (1: no gaps);
+ *   capacity > 0: the layer's own layout, expert e from e * C_stride on (C_stride = capacity rounded up to 128), pairs behind
+ *                 an expert's first `capacity` dropped; `align` has to be 128.  counts is then what etr_expert_ffn reads.
+ * Rows of an expert behind its last, up to the next multiple of `align`, are pad rows: etr_sort_rows and
+ * etr_unsort_rows_bwd write zeros there.  Rows behind those are left as they are.
+ * Requirements: T >= 0 (0: nothing but the plan's zeros is written), 1 <= k <= ETR_SORT_MAX_K, 1 <= E <= ETR_SORT_MAX_E,
+ * d % 8 == 0, 1 <= align <= 1024, T*k and the buffers' rows below 2^31 - 65536; pointers 16-byte aligned.  No output may
+ * overlap an input. */
+#define ETR_SORT_MAX_K 32
+#define ETR_SORT_MAX_E 1024
+typedef struct etr_sort_config {
+  int32_t T, k, E, d;
+  int32_t dtype;              /* etr_dtype of the token rows; weights are fp32 */
+  int32_t align, capacity;
+  int32_t reserved0;
+} etr_sort_config;
+
+/* The plan of one choice (host struct of device pointers), written by etr_sort, read by the row passes. */
+typedef struct etr_sort_plan {
+  int32_t* counts;            /* [E]    rows of each expert */
+  int32_t* offsets;           /* [E+1]  first row of each expert; offsets[E]: the end of the last one's rows, pad rows included */
+  int32_t* totals;            /* [4]    pairs with a row, pairs dropped, pairs without an expert, 0 */
+  int32_t* row_token;         /* [etr_sort_n_rows] token of each row, -1 where there is none */
+  int32_t* pos;               /* [T,k]  row of each pair, -1 where there is none */
+} etr_sort_plan;
+
+etr_status etr_sort_validate(const etr_sort_config* cfg);
+/* Rows of a buffer that holds any choice of this configuration: T*k + min(E, T*k) (align - 1), or E * C_stride. */
+int64_t etr_sort_n_rows(const etr_sort_config* cfg);
+/* Size of a block for the plan (need, may be NULL) and its carving (out, may be NULL; base 256-byte aligned). */
+etr_status etr_sort_plan_bind(const etr_sort_config* cfg, void* base, size_t bytes, etr_sort_plan* out, size_t* need);
+/* topk_idx [T,k] int32.  Fills every member of the plan.  One launch. */
+etr_status etr_sort(const etr_sort_config* cfg, const int32_t* topk_idx, const etr_sort_plan* plan, void* stream);
+/* Xs[pos[t][j],:] = X[t,:]; pad rows 0. */
+etr_status etr_sort_rows(const etr_sort_config* cfg, const void* X, const etr_sort_plan* plan, void* Xs, void* stream);
+/* dX[t,:] = sum_j dXs[pos[t][j],:]  (0 for a token without rows; overwrites dX). */
+etr_status etr_sort_rows_bwd(const etr_sort_config* cfg, const void* dXs, const etr_sort_plan* plan, void* dX, void* stream);
+/* Y[t,:] = sum_j weights[t][j] O[pos[t][j],:]  (0 for a token without rows).  Sums in fp32, j ascending. */
+etr_status etr_unsort_rows(const etr_sort_config* cfg, const void* O, const float* weights, const etr_sort_plan* plan, void* Y,
+                           void* stream);
+/* dO[pos[t][j],:] = weights[t][j] dY[t,:], pad rows 0;  dweights[t][j] = <dY[t,:], O[pos[t][j],:]>, 0 without a row. */
+etr_status etr_unsort_rows_bwd(const etr_sort_config* cfg, const void* dY, const void* O, const float* weights,
+                               const etr_sort_plan* plan, void* dO, float* dweights, void* stream);
+
+/* ---- the norm before a block and the join behind it ------------------------------------------------- */
+
+/* Rows of d values (d % 8 == 0, d <= ETR_NORM_MAX_D) of `dtype`; gains, gates, 1/rms and their gradients fp32; pointers 16-byte
+ * aligned.  r(x) = 1 / sqrt(mean x^2 + eps), eps > 0.  A NULL gain or gate means ones.  T = 0 writes zero weight gradients
+ * and nothing else.  Values below 1e18 in size (their squares are summed in fp32).
+ * Xo may be X, and dX may be dXo or dres (the residual stream updated in place); no other output may overlap an input. */
+#define ETR_NORM_MAX_D 16384
+typedef struct etr_norm_config {
+  int32_t T, d;
+  int32_t dtype;
+  int32_t post_norm;          /* join: != 0: the block's output is normed before its gain */
+  float eps;
+  float res_scale;            /* join: a, the factor of the residual */
+  float branch_scale;         /* join: b, the factor of the block's output */
+  int32_t reserved0;
+} etr_norm_config;
+
+etr_status etr_norm_validate(const etr_norm_config* cfg);
+/* Scratch of the two backward calls: partial sums of the gains' gradients (does not depend on T). */
+etr_status etr_norm_workspace_bytes(const etr_norm_config* cfg, size_t* bytes);
+
+/* N[t,:] = X[t,:] r(X[t]) w;  rstd[t] = r(X[t]) (NULL: not wanted). */
+etr_status etr_prenorm(const etr_norm_config* cfg, const void* X, const float* w, void* N, float* rstd, void* stream);
+/* With xh = X rstd and g = w dN:  dX = dres + rstd (g - xh <g, xh> / d),  dw = sum_t dN xh.  dres (NULL: zeros) is the gradient
+ * that comes along the residual; dw and ws may both be NULL. */
+etr_status etr_prenorm_bwd(const etr_norm_config* cfg, const void* dN, const void* X, const float* w, const float* rstd,
+                           const void* dres, void* dX, float* dw, void* ws, void* stream);
+/* X residual, Y the block's output, gate [T]:
+ *   Xo = a X + b gate w_post (Y r(Y), or Y without post_norm);  N = Xo r(Xo) w_next
+ * N NULL: no next norm (w_next and rstd_o are not used).  N is the norm of the fp32 sum before it is rounded to Xo.
+ * rstd_y = r(Y) and rstd_o = r(Xo) are what the backward pass reads (NULL: not wanted). */
+etr_status etr_join(const etr_norm_config* cfg, const void* X, const void* Y, const float* w_post, const float* gate,
+                    const float* w_next, void* Xo, void* N, float* rstd_y, float* rstd_o, void* stream);
+/* From dXo (the sum's gradient from later in the residual stream) and dN, either of which may be NULL, with Y and Xo as the forward
+ * call read and wrote them: the gradients of X, Y, w_post, gate and w_next (the last three may be NULL; ws may be NULL
+ * where no gain's gradient is wanted).  Xo, w_next and rstd_o are used only with dN, rstd_y only with post_norm. */
+etr_status etr_join_bwd(const etr_norm_config* cfg, const void* dXo, const void* dN, const void* Y, const void* Xo,
+                        const float* w_post, const float* gate, const float* w_next, const float* rstd_y, const float* rstd_o,
+                        void* dX, void* dY, float* dw_post, float* dgate, float* dw_next, void* ws, void* stream);
+
 /* Number of kernels launched by this library in the calling process so far. */
 int64_t etr_launch_count(void);
 

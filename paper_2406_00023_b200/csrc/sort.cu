@@ -1,0 +1,376 @@
+// Tokens sorted by the expert a caller chose for them, and back: the plan (which row every (token, choice) pair takes) and
+// the four row passes.  Stable: the rows of an expert hold its pairs in ascending (token, choice) order.
+#include <cooperative_groups.h>
+
+#include "common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace etr {
+
+constexpr int SORT_WARPS = 16;
+constexpr int SORT_MAX_CLUSTER = 8;
+constexpr int SORT_MAX_E = 1024;
+
+struct SortShape {
+  int N, k, E, align, capacity, stride, n_rows;      // stride: rows between experts in the capacity form, else 0
+};
+
+// The plan, by one cluster.  Every warp owns a run of consecutive pairs and counts its ids per expert (shared memory), the
+// warps' counts become prefix sums within the CTA and, through distributed shared memory, across the cluster; the row
+// of a pair is then its expert's start, plus the pairs of earlier warps, plus those before it in its own warp (one
+// match over the warp's 32 ids a round).  No atomics decide an order, so the plan is stable and the same every time.
+__global__ void __launch_bounds__(SORT_WARPS * 32)
+sort_plan_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+                 int32_t* __restrict__ totals, int32_t* __restrict__ row_token, int32_t* __restrict__ pos) {
+  extern __shared__ int sm[];
+  int* wc = sm;                                  // [SORT_WARPS][E] pairs of this warp, then of the warps before it
+  int* mine = wc + SORT_WARPS * s.E;             // [E] pairs of this CTA
+  int* start = mine + s.E;                       // [E] first row of the expert
+  int* kept = start + s.E;                       // [E]
+  __shared__ int s_warp[SORT_WARPS], s_found[SORT_WARPS], s_kept[SORT_WARPS];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = (int)cluster.block_rank(), ncta = (int)cluster.num_blocks();
+  for (int i = tid; i < SORT_WARPS * s.E; i += SORT_WARPS * 32) wc[i] = 0;
+  grid_sync();
+  __syncthreads();
+  const int runs = ncta * SORT_WARPS;
+  const int run = ((s.N + runs - 1) / runs + 31) & ~31;            // pairs per warp, whole rounds of 32
+  const long long beg = (long long)(rank * SORT_WARPS + warp) * run;
+  const int n = (int)max(0ll, min((long long)run, (long long)s.N - beg));
+  int* cnt = wc + warp * s.E;
+  for (int i = lane; i < n; i += 32) {
+    const int e = ids[beg + i];
+    if ((unsigned)e < (unsigned)s.E) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  for (int e = tid; e < s.E; e += SORT_WARPS * 32) {
+    int acc = 0;
+    for (int w = 0; w < SORT_WARPS; ++w) { const int c = wc[w * s.E + e]; wc[w * s.E + e] = acc; acc += c; }
+    mine[e] = acc;
+  }
+  cluster.sync();
+  // Experts [2 tid, 2 tid + 2): pairs found, kept, and rows taken; the starts by a scan over the CTA's threads.
+  int rows[2] = {0, 0}, found = 0, keeps = 0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int e = 2 * tid + u;
+    if (e >= s.E) break;
+    int all = 0, before = 0;
+    for (int c = 0; c < ncta; ++c) {
+      const int v = cluster.map_shared_rank(mine, c)[e];
+      all += v;
+      before += c < rank ? v : 0;
+    }
+    const int keep = s.capacity ? min(all, s.capacity) : all;
+    for (int w = 0; w < SORT_WARPS; ++w) wc[w * s.E + e] += before;
+    kept[e] = keep;
+    found += all;
+    keeps += keep;
+    rows[u] = s.capacity ? s.stride : (keep + s.align - 1) / s.align * s.align;
+    if (rank == 0) counts[e] = keep;
+  }
+  int inc = rows[0] + rows[1];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    found += __shfl_xor_sync(0xffffffffu, found, o);
+    keeps += __shfl_xor_sync(0xffffffffu, keeps, o);
+  }
+  if (lane == 31) { s_warp[warp] = inc; s_found[warp] = found; s_kept[warp] = keeps; }
+  __syncthreads();
+  int at = inc - rows[0] - rows[1], end = 0;
+  found = keeps = 0;
+  for (int w = 0; w < SORT_WARPS; ++w) {
+    at += w < warp ? s_warp[w] : 0;
+    end += s_warp[w];
+    found += s_found[w];
+    keeps += s_kept[w];
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int e = 2 * tid + u;
+    if (e < s.E) {
+      start[e] = at;
+      if (rank == 0) offsets[e] = at;
+    }
+    at += rows[u];
+  }
+  if (rank == 0 && tid == 0) {
+    offsets[s.E] = end;
+    totals[0] = keeps; totals[1] = found - keeps; totals[2] = s.N - found; totals[3] = 0;
+  }
+  __syncthreads();
+  const int limit = s.capacity ? s.capacity : s.N;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const int i = i0 + lane;
+    const int e = i < n ? ids[beg + i] : -1;
+    const bool ok = (unsigned)e < (unsigned)s.E;
+    const unsigned same = __match_any_sync(0xffffffffu, ok ? e : -1);
+    int r = 0;
+    if (ok) r = cnt[e] + __popc(same & ((1u << lane) - 1u));
+    __syncwarp();
+    if (ok && (same >> lane) == 1u) cnt[e] = r + 1;           // the last of its kind in this round
+    __syncwarp();
+    if (i < n) {
+      const int row = ok && r < limit ? start[e] + r : -1;
+      pos[beg + i] = row;
+      if (row >= 0) row_token[row] = (int)((beg + i) / s.k);
+    }
+  }
+  // rows without a token
+  for (int e = rank; e < s.E; e += ncta) {
+    const int stop = e + 1 < s.E ? start[e + 1] : s.n_rows;
+    for (int r = start[e] + kept[e] + tid; r < stop; r += SORT_WARPS * 32) row_token[r] = -1;
+  }
+  cluster.sync();                                // no CTA leaves while another may still read its counts
+}
+
+// Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first PAD_SHARES * E blocks of a
+// row pass write them, so that they do not end up as its tail.
+constexpr int PAD_SHARES = 8;
+__device__ __forceinline__ void zero_pad_rows(uint4* rows, int nv, const int32_t* counts, const int32_t* offsets, int align) {
+  const int e = blockIdx.x / PAD_SHARES, share = blockIdx.x % PAD_SHARES;
+  const int c = counts[e], pads = (c + align - 1) / align * align - c;
+  uint4* dst = rows + ((size_t)offsets[e] + c) * nv;
+  const size_t n = (size_t)pads * nv;
+  for (size_t v = share * 256 + threadIdx.x; v < n; v += PAD_SHARES * 256) dst[v] = make_uint4(0, 0, 0, 0);
+}
+
+// Xs[pos[t][j]] = X[t].  Token-major, so that a token is read once however many experts it has.  X is a flat run of
+// 16-byte pieces; a block takes SORT_PIECES of them.
+constexpr int SORT_UNROLL = 4, SORT_PIECES = 256 * SORT_UNROLL;
+__global__ void __launch_bounds__(256)
+sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, const int32_t* offsets, uint4* __restrict__ Xs, long long n,
+                 int nv, int k, int align, int pad_blocks) {
+  grid_sync();
+  if ((int)blockIdx.x < pad_blocks) return zero_pad_rows(Xs, nv, counts, offsets, align);
+  const long long base = (long long)(blockIdx.x - pad_blocks) * SORT_PIECES;
+  const long long t0 = base / nv;
+  const int r0 = (int)(base - t0 * nv);
+  uint4 q[SORT_UNROLL];
+#pragma unroll
+  for (int u = 0; u < SORT_UNROLL; ++u) {
+    const long long i = base + u * 256 + threadIdx.x;
+    if (i < n) q[u] = X[i];
+  }
+#pragma unroll
+  for (int u = 0; u < SORT_UNROLL; ++u) {
+    const int i = u * 256 + (int)threadIdx.x;
+    if (base + i >= n) break;
+    const unsigned dt = (unsigned)(r0 + i) / (unsigned)nv;
+    const int v = r0 + i - (int)dt * nv;
+    const int32_t* p = pos + (t0 + dt) * k;
+    for (int j = 0; j < k; ++j) {
+      const int row = p[j];
+      if (row >= 0) Xs[(size_t)row * nv + v] = q[u];
+    }
+  }
+}
+
+// Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.
+template <class T>
+__global__ void __launch_bounds__(256)
+unsort_kernel(const T* rows, const float* w, const int32_t* pos, T* __restrict__ Y, long long n, int ng, int k, int d) {
+  grid_sync();
+  const long long base = (long long)blockIdx.x * 256;
+  const long long t0 = base / ng;
+  const int i = (int)(base - t0 * ng) + (int)threadIdx.x;
+  if (base + (int)threadIdx.x >= n) return;
+  const unsigned dt = (unsigned)i / (unsigned)ng;
+  const int g = i - (int)dt * ng;
+  const long long t = t0 + dt;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < k; ++j) {
+    const int row = pos[t * k + j];
+    if (row < 0) continue;
+    const float f = w ? w[t * k + j] : 1.f;
+    const Vec8<T> o = Vec8<T>::load(rows + (size_t)row * d + (size_t)g * 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(f, o.v[e], acc[e]);
+  }
+  Vec8<T>::store(Y + (size_t)t * d + (size_t)g * 8, acc);
+}
+
+// dO[pos[t][j]] = w[t][j] dY[t], dw[t][j] = <dY[t], O[pos[t][j]]>; a warp per pair.  The warps of a token are neighbours, so its
+// dY comes from HBM once.
+template <class T>
+__global__ void __launch_bounds__(256)
+unsort_bwd_kernel(const T* dY, const T* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
+                  T* __restrict__ dO, float* __restrict__ dw, long long pairs, int k, int d, int align, int pad_blocks) {
+  grid_sync();
+  if ((int)blockIdx.x < pad_blocks)
+    return zero_pad_rows(reinterpret_cast<uint4*>(dO), d * (int)sizeof(T) / 16, counts, offsets, align);
+  const long long i = (long long)(blockIdx.x - pad_blocks) * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (i >= pairs) return;
+  const int row = pos[i];
+  if (row < 0) {
+    if (lane == 0) dw[i] = 0.f;
+    return;
+  }
+  const float f = w[i];
+  const T* gy = dY + (size_t)(i / k) * d;
+  const T* o = O + (size_t)row * d;
+  T* out = dO + (size_t)row * d;
+  float dot = 0.f;
+  for (int v = lane; v < d / 8; v += 32) {
+    const Vec8<T> a = Vec8<T>::load(gy + v * 8), b = Vec8<T>::load(o + v * 8);
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { r[e] = f * a.v[e]; dot = fmaf(a.v[e], b.v[e], dot); }
+    Vec8<T>::store(out + v * 8, r);
+  }
+  dot = warp_sum(dot);
+  if (lane == 0) dw[i] = dot;
+}
+
+// ---- launches ----------------------------------------------------------------------------------
+static int sort_stride(const etr_sort_config* c) { return c->capacity ? (c->capacity + 127) / 128 * 128 : 0; }
+
+static long long sort_rows_bound(const etr_sort_config* c) {
+  if (c->capacity) return (long long)c->E * ((c->capacity + 127ll) / 128 * 128);
+  const long long n = (long long)c->T * c->k;
+  return n + (n < c->E ? n : c->E) * (long long)(c->align - 1);
+}
+
+static etr_status sort_valid(const etr_sort_config* c) {
+  if (c == nullptr) return ETR_ERR_ARG;
+  if (c->T < 0 || c->k < 1 || c->E < 1 || c->d < 1 || c->align < 1 || c->capacity < 0) return ETR_ERR_ARG;
+  if (c->dtype != ETR_F32 && c->dtype != ETR_BF16) return ETR_ERR_ARG;
+  if (c->k > ETR_SORT_MAX_K || c->E > ETR_SORT_MAX_E || c->d % 8 != 0 || c->align > 1024) return ETR_ERR_SHAPE;
+  if (c->capacity && c->align != 128) return ETR_ERR_SHAPE;
+  if ((long long)c->T * c->k >= (1ll << 31) - 65536 || sort_rows_bound(c) >= (1ll << 31) - 65536) return ETR_ERR_SHAPE;
+  return ETR_OK;
+}
+
+static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* p, std::initializer_list<const void*> more) {
+  if (p == nullptr || p->counts == nullptr || p->offsets == nullptr || p->totals == nullptr) return ETR_ERR_ARG;
+  const bool rows = sort_rows_bound(c) > 0, some = c->T > 0;
+  if ((rows && p->row_token == nullptr) || (some && p->pos == nullptr)) return ETR_ERR_ARG;
+  for (const void* q : {(const void*)p->counts, (const void*)p->offsets, (const void*)p->totals, (const void*)p->row_token, (const void*)p->pos})
+    if (!aligned16(q)) return ETR_ERR_ALIGN;
+  if (!some) return ETR_OK;                  // nothing is read or written through them
+  for (const void* q : more) {
+    if (q == nullptr) return ETR_ERR_ARG;
+    if (!aligned16(q)) return ETR_ERR_ALIGN;
+  }
+  return ETR_OK;
+}
+
+static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD_SHARES * c->E : 0; }
+
+static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
+  static std::atomic<unsigned long long> done{0};
+  const size_t smem = (size_t)(SORT_WARPS + 3) * c->E * 4;
+  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 3) * SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  const SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c)};
+  int ncta = 1;
+  while (ncta < SORT_MAX_CLUSTER && s.N > ncta * SORT_WARPS * 64) ncta *= 2;
+  ETR_TIME_BEGIN("sort_plan_kernel");
+  launch_kernel(sort_plan_kernel, ncta, SORT_WARPS * 32, smem, st, ncta, ids, s, p->counts, p->offsets, p->totals, p->row_token, p->pos);
+  ETR_LAUNCH_CHECK();
+  return ETR_OK;
+}
+
+template <class T>
+static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_plan* p, const void* a, const void* b, const float* w,
+                            void* out, float* dw, cudaStream_t st) {
+  const int pad = sort_pad_blocks(c), nv = c->d * (int)sizeof(T) / 16, ng = c->d / 8;
+  const long long n = (long long)c->T * (which == 0 ? nv : ng), pairs = (long long)c->T * c->k;
+  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 255) / 256 : (pairs + 7) / 8;
+  if (blocks + pad >= (1ll << 31)) return ETR_ERR_SHAPE;
+  switch (which) {
+    case 0:
+      ETR_TIME_BEGIN("sort_rows_kernel");
+      launch_kernel(sort_rows_kernel, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, p->pos, p->counts, p->offsets, (uint4*)out, n,
+                    nv, c->k, c->align, pad);
+      break;
+    case 1:
+      ETR_TIME_BEGIN("unsort_kernel");
+      launch_kernel(unsort_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const T*)a, w, p->pos, (T*)out, n, ng, c->k, c->d);
+      break;
+    case 2:
+      ETR_TIME_BEGIN("unsort_bwd_kernel");
+      launch_kernel(unsort_bwd_kernel<T>, (unsigned)(blocks + pad), 256, 0, st, 1, (const T*)a, (const T*)b, w, p->pos, p->counts,
+                    p->offsets, (T*)out, dw, pairs, c->k, c->d, c->align, pad);
+      break;
+  }
+  ETR_LAUNCH_CHECK();
+  return ETR_OK;
+}
+
+static etr_status sort_pass_typed(int which, const etr_sort_config* c, const etr_sort_plan* p, const void* a, const void* b, const float* w,
+                                  void* out, float* dw, cudaStream_t st) {
+  if (c->T == 0) return ETR_OK;
+  return c->dtype == ETR_BF16 ? sort_pass<__nv_bfloat16>(which, c, p, a, b, w, out, dw, st) : sort_pass<float>(which, c, p, a, b, w, out, dw, st);
+}
+
+}  // namespace etr
+
+using namespace etr;
+
+extern "C" {
+
+etr_status etr_sort_validate(const etr_sort_config* c) { return sort_valid(c); }
+
+int64_t etr_sort_n_rows(const etr_sort_config* c) { return sort_valid(c) == ETR_OK ? sort_rows_bound(c) : 0; }
+
+etr_status etr_sort_plan_bind(const etr_sort_config* c, void* base, size_t bytes, etr_sort_plan* out, size_t* need) {
+  ETR_TRY(sort_valid(c));
+  if (need == nullptr && out == nullptr) return ETR_ERR_ARG;
+  if (out && base == nullptr) return ETR_ERR_ARG;
+  if (out && (reinterpret_cast<uintptr_t>(base) & 255u)) return ETR_ERR_ALIGN;
+  size_t off = 0;
+  auto take = [&](size_t n) { char* q = (char*)base + off; off = align_up(off + n * 4, 256); return (int32_t*)q; };
+  etr_sort_plan p;
+  p.counts = take(c->E);
+  p.offsets = take(c->E + 1);
+  p.totals = take(4);
+  p.row_token = take((size_t)sort_rows_bound(c));
+  p.pos = take((size_t)c->T * c->k);
+  if (need) *need = off;
+  if (out) {
+    if (bytes < off) return ETR_ERR_WORKSPACE;
+    *out = p;
+  }
+  return ETR_OK;
+}
+
+etr_status etr_sort(const etr_sort_config* c, const int32_t* topk_idx, const etr_sort_plan* plan, void* stream) {
+  ETR_TRY(sort_valid(c));
+  ETR_TRY(sort_plan_ptrs(c, plan, {topk_idx}));
+  return plan_launch(c, topk_idx, plan, (cudaStream_t)stream);
+}
+
+etr_status etr_sort_rows(const etr_sort_config* c, const void* X, const etr_sort_plan* plan, void* Xs, void* stream) {
+  ETR_TRY(sort_valid(c));
+  ETR_TRY(sort_plan_ptrs(c, plan, {X, Xs}));
+  return sort_pass_typed(0, c, plan, X, nullptr, nullptr, Xs, nullptr, (cudaStream_t)stream);
+}
+
+etr_status etr_sort_rows_bwd(const etr_sort_config* c, const void* dXs, const etr_sort_plan* plan, void* dX, void* stream) {
+  ETR_TRY(sort_valid(c));
+  ETR_TRY(sort_plan_ptrs(c, plan, {dXs, dX}));
+  return sort_pass_typed(1, c, plan, dXs, nullptr, nullptr, dX, nullptr, (cudaStream_t)stream);
+}
+
+etr_status etr_unsort_rows(const etr_sort_config* c, const void* O, const float* weights, const etr_sort_plan* plan, void* Y, void* stream) {
+  ETR_TRY(sort_valid(c));
+  ETR_TRY(sort_plan_ptrs(c, plan, {O, weights, Y}));
+  return sort_pass_typed(1, c, plan, O, nullptr, weights, Y, nullptr, (cudaStream_t)stream);
+}
+
+etr_status etr_unsort_rows_bwd(const etr_sort_config* c, const void* dY, const void* O, const float* weights, const etr_sort_plan* plan,
+                               void* dO, float* dweights, void* stream) {
+  ETR_TRY(sort_valid(c));
+  ETR_TRY(sort_plan_ptrs(c, plan, {dY, O, weights, dO, dweights}));
+  return sort_pass_typed(2, c, plan, dY, O, weights, dO, dweights, (cudaStream_t)stream);
+}
+
+}  // extern "C"

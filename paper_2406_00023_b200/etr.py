@@ -30,6 +30,9 @@ EXPORTS = [
     "etr_layer_forward", "etr_layer_backward", "etr_layer_step_host", "etr_layer_step_host_begin",
     "etr_layer_step_host_wait", "etr_read_stats", "etr_selftest_bounded_wait",
     "etr_launch_count", "etr_timing_enable", "etr_timing_collect",
+    "etr_sort_validate", "etr_sort_n_rows", "etr_sort_plan_bind", "etr_sort", "etr_sort_rows", "etr_sort_rows_bwd",
+    "etr_unsort_rows", "etr_unsort_rows_bwd",
+    "etr_norm_validate", "etr_norm_workspace_bytes", "etr_prenorm", "etr_prenorm_bwd", "etr_join", "etr_join_bwd",
 ]
 
 
@@ -92,6 +95,12 @@ def lib():
         l.etr_status_string.argtypes = [C.c_int]
         l.etr_launch_count.restype = C.c_int64
         l.etr_c_stride.restype = C.c_int32
+        l.etr_sort_n_rows.restype = C.c_int64
+        for name, n in (("etr_sort", 4), ("etr_sort_rows", 5), ("etr_sort_rows_bwd", 5), ("etr_unsort_rows", 6),
+                        ("etr_unsort_rows_bwd", 8), ("etr_prenorm", 6), ("etr_prenorm_bwd", 10), ("etr_join", 11),
+                        ("etr_join_bwd", 17)):
+            getattr(l, name).argtypes = [C.c_void_p] * n
+        l.etr_sort_plan_bind.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         _lib = l
     return _lib
 
@@ -375,3 +384,171 @@ def layer_step_host(cfg, X_host, dY_host, R, W1g, W1u, W2, buf: LayerBuffers, Y_
     _check(lib().etr_layer_step_host(C.byref(cfg), _p(X_host), _p(dY_host), _p(R), _p(W1g), _p(W1u),
                                      _p(W2), C.byref(buf.c), _p(Y_host), _p(dX_host), _p(dR),
                                      _p(dW1g), _p(dW1u), _p(dW2), _stream()), "etr_layer_step_host")
+
+
+# ---- tokens sorted by a choice of experts that the caller made -------------------------------------
+class SortConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "k", "E", "d", "dtype", "align", "capacity", "reserved0")]
+
+
+class SortPlan(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("counts", "offsets", "totals", "row_token", "pos")]
+
+
+SORT_MAX_K, SORT_MAX_E, NORM_MAX_D = 32, 1024, 16384
+
+
+def make_sort_config(*, T, k, E, d, dtype, align=1, capacity=0) -> SortConfig:
+    return SortConfig(T=T, k=k, E=E, d=d, dtype=int(dtype), align=align, capacity=capacity, reserved0=0)
+
+
+def sort_validate(cfg: SortConfig) -> int:
+    return lib().etr_sort_validate(C.byref(cfg))
+
+
+def sort_n_rows(cfg: SortConfig) -> int:
+    return lib().etr_sort_n_rows(C.byref(cfg))
+
+
+class SortBuffers:
+    """The plan of a choice: one device block carved by etr_sort_plan_bind, with typed views of each member."""
+
+    def __init__(self, cfg: SortConfig, device="cuda"):
+        n = C.c_size_t(0)
+        _check(lib().etr_sort_plan_bind(C.byref(cfg), None, C.c_size_t(0), None, C.byref(n)), "etr_sort_plan_bind")
+        self.cfg, self.n_rows = cfg, sort_n_rows(cfg)
+        self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
+        base = (self.block.data_ptr() + 255) // 256 * 256
+        self.c = SortPlan()
+        _check(lib().etr_sort_plan_bind(C.byref(cfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_sort_plan_bind")
+        for name, shape in (("counts", (cfg.E,)), ("offsets", (cfg.E + 1,)), ("totals", (4,)), ("row_token", (self.n_rows,)),
+                            ("pos", (cfg.T, cfg.k))):
+            off, count = (getattr(self.c, name) or base) - self.block.data_ptr(), 1
+            for m in shape:
+                count *= m
+            setattr(self, name, self.block[off:off + 4 * count].view(torch.int32).view(shape))
+        self.ptr = C.addressof(self.c)
+
+
+def _arg(where, t, dtype, n, device, optional=False):
+    """Address of a tensor after the checks that addresses alone do not allow: its type, place, order and size."""
+    if t is None:
+        if not optional:
+            raise EtrError(ERR_ARG, where)
+        return None
+    if t.dtype is not dtype or t.device != device:
+        raise EtrError(ERR_ARG, f"{where}: a {t.dtype} tensor on {t.device}, {dtype} on {device} is wanted")
+    if t.numel() != n or not t.is_contiguous():
+        raise EtrError(ERR_SHAPE, f"{where}: a tensor of shape {tuple(t.shape)}, {n} contiguous elements are wanted")
+    return t.data_ptr()
+
+
+def _call_device(where, t):
+    """Device and stream of a call: those of the current device, on which its first tensor has to be."""
+    d = t.device
+    if d.type != "cuda" or d.index != torch.cuda.current_device():
+        raise EtrError(ERR_ARG, f"{where}: a tensor on {d}, which is not the current CUDA device")
+    return d, torch.cuda.current_stream().cuda_stream
+
+
+def sort(cfg, topk_idx, plan: SortBuffers):
+    d, st = _call_device("etr_sort", plan.block)
+    _check(lib().etr_sort(C.addressof(cfg), _arg("etr_sort", topk_idx, torch.int32, cfg.T * cfg.k, d), plan.ptr, st), "etr_sort")
+
+
+def sort_rows(cfg, X, plan: SortBuffers, Xs):
+    w, act = "etr_sort_rows", torch_dtype(cfg)
+    d, st = _call_device(w, plan.block)
+    _check(lib().etr_sort_rows(C.addressof(cfg), _arg(w, X, act, cfg.T * cfg.d, d), plan.ptr,
+                               _arg(w, Xs, act, plan.n_rows * cfg.d, d), st), w)
+
+
+def sort_rows_bwd(cfg, dXs, plan: SortBuffers, dX):
+    w, act = "etr_sort_rows_bwd", torch_dtype(cfg)
+    d, st = _call_device(w, plan.block)
+    _check(lib().etr_sort_rows_bwd(C.addressof(cfg), _arg(w, dXs, act, plan.n_rows * cfg.d, d), plan.ptr,
+                                   _arg(w, dX, act, cfg.T * cfg.d, d), st), w)
+
+
+def unsort_rows(cfg, O, weights, plan: SortBuffers, Y):
+    w, act = "etr_unsort_rows", torch_dtype(cfg)
+    d, st = _call_device(w, plan.block)
+    _check(lib().etr_unsort_rows(C.addressof(cfg), _arg(w, O, act, plan.n_rows * cfg.d, d),
+                                 _arg(w, weights, torch.float32, cfg.T * cfg.k, d), plan.ptr,
+                                 _arg(w, Y, act, cfg.T * cfg.d, d), st), w)
+
+
+def unsort_rows_bwd(cfg, dY, O, weights, plan: SortBuffers, dO, dweights):
+    w, act = "etr_unsort_rows_bwd", torch_dtype(cfg)
+    d, st = _call_device(w, plan.block)
+    _check(lib().etr_unsort_rows_bwd(C.addressof(cfg), _arg(w, dY, act, cfg.T * cfg.d, d), _arg(w, O, act, plan.n_rows * cfg.d, d),
+                                     _arg(w, weights, torch.float32, cfg.T * cfg.k, d), plan.ptr,
+                                     _arg(w, dO, act, plan.n_rows * cfg.d, d),
+                                     _arg(w, dweights, torch.float32, cfg.T * cfg.k, d), st), w)
+
+
+# ---- the norm before a block and the join behind it -------------------------------------------------
+class NormConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("T", "d", "dtype", "post_norm")] + \
+               [(n, C.c_float) for n in ("eps", "res_scale", "branch_scale")] + [("reserved0", C.c_int32)]
+
+
+def make_norm_config(*, T, d, dtype, eps=1e-6, res_scale=1.0, branch_scale=1.0, post_norm=False) -> NormConfig:
+    return NormConfig(T=T, d=d, dtype=int(dtype), post_norm=int(bool(post_norm)), eps=float(eps), res_scale=float(res_scale),
+                      branch_scale=float(branch_scale), reserved0=0)
+
+
+def norm_validate(cfg: NormConfig) -> int:
+    return lib().etr_norm_validate(C.byref(cfg))
+
+
+def norm_workspace_bytes(cfg: NormConfig) -> int:
+    n = C.c_size_t(0)
+    _check(lib().etr_norm_workspace_bytes(C.byref(cfg), C.byref(n)), "etr_norm_workspace_bytes")
+    return n.value
+
+
+def _norm_ws(where, cfg, ws, device):
+    if ws is None:
+        return None
+    if ws.device != device or not ws.is_contiguous():
+        raise EtrError(ERR_ARG, f"{where}: the workspace")
+    if ws.numel() * ws.element_size() < norm_workspace_bytes(cfg):
+        raise EtrError(ERR_WORKSPACE, where)
+    return ws.data_ptr()
+
+
+def prenorm(cfg, X, w, N, rstd=None):
+    f, act, n = "etr_prenorm", torch_dtype(cfg), cfg.T * cfg.d
+    d, st = _call_device(f, X)
+    _check(lib().etr_prenorm(C.addressof(cfg), _arg(f, X, act, n, d), _arg(f, w, torch.float32, cfg.d, d, True),
+                             _arg(f, N, act, n, d), _arg(f, rstd, torch.float32, cfg.T, d, True), st), f)
+
+
+def prenorm_bwd(cfg, dN, X, w, rstd, dres, dX, dw, ws):
+    f, act, f32, n = "etr_prenorm_bwd", torch_dtype(cfg), torch.float32, cfg.T * cfg.d
+    d, st = _call_device(f, X)
+    _check(lib().etr_prenorm_bwd(C.addressof(cfg), _arg(f, dN, act, n, d), _arg(f, X, act, n, d), _arg(f, w, f32, cfg.d, d, True),
+                                 _arg(f, rstd, f32, cfg.T, d), _arg(f, dres, act, n, d, True), _arg(f, dX, act, n, d),
+                                 _arg(f, dw, f32, cfg.d, d, True), _norm_ws(f, cfg, ws, d), st), f)
+
+
+def join(cfg, X, Y, w_post, gate, w_next, Xo, N, rstd_y=None, rstd_o=None):
+    f, act, f32, n = "etr_join", torch_dtype(cfg), torch.float32, cfg.T * cfg.d
+    d, st = _call_device(f, X)
+    _check(lib().etr_join(C.addressof(cfg), _arg(f, X, act, n, d), _arg(f, Y, act, n, d), _arg(f, w_post, f32, cfg.d, d, True),
+                          _arg(f, gate, f32, cfg.T, d, True), _arg(f, w_next, f32, cfg.d, d, True), _arg(f, Xo, act, n, d),
+                          _arg(f, N, act, n, d, True), _arg(f, rstd_y, f32, cfg.T, d, True),
+                          _arg(f, rstd_o, f32, cfg.T, d, True), st), f)
+
+
+def join_bwd(cfg, dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws):
+    f, act, f32, n = "etr_join_bwd", torch_dtype(cfg), torch.float32, cfg.T * cfg.d
+    d, st = _call_device(f, Y)
+    _check(lib().etr_join_bwd(C.addressof(cfg), _arg(f, dXo, act, n, d, True), _arg(f, dN, act, n, d, True), _arg(f, Y, act, n, d),
+                              _arg(f, Xo, act, n, d, True), _arg(f, w_post, f32, cfg.d, d, True),
+                              _arg(f, gate, f32, cfg.T, d, True), _arg(f, w_next, f32, cfg.d, d, True),
+                              _arg(f, rstd_y, f32, cfg.T, d, True), _arg(f, rstd_o, f32, cfg.T, d, True),
+                              _arg(f, dX, act, n, d), _arg(f, dY, act, n, d), _arg(f, dw_post, f32, cfg.d, d, True),
+                              _arg(f, dgate, f32, cfg.T, d, True), _arg(f, dw_next, f32, cfg.d, d, True),
+                              _norm_ws(f, cfg, ws, d), st), f)

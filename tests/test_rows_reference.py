@@ -1,0 +1,215 @@
+"""The 64-bit definitions that the GPU tests hold the row operators to: gradients against central differences of the forward
+forms, and the refusals of the C entry points, none of which need a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from tests import rows_reference as rr
+from paper_2406_00023_b200 import etr
+
+F64 = torch.float64
+
+
+def differences(f, x, step=1e-5):
+    """Gradient of the scalar f by central differences."""
+    g = torch.zeros_like(x)
+    for i in range(x.numel()):
+        keep = float(x.view(-1)[i])
+        x.view(-1)[i] = keep + step
+        up = float(f())
+        x.view(-1)[i] = keep - step
+        down = float(f())
+        x.view(-1)[i] = keep
+        g.view(-1)[i] = (up - down) / (2 * step)
+    return g
+
+
+def close(got, ref):
+    assert torch.allclose(got, ref, rtol=1e-6, atol=1e-7), float((got - ref).abs().max())
+
+
+@pytest.mark.parametrize("gain", [True, False])
+def test_prenorm_gradient_is_the_forward_forms_slope(gain):
+    g = torch.Generator().manual_seed(1)
+    x, dN, dres = (torch.randn(3, 8, generator=g, dtype=F64) for _ in range(3))
+    w = torch.randn(8, generator=g, dtype=F64) if gain else None
+    f = lambda: (rr.prenorm(x, w, 1e-3, torch.float64)[0][0] * dN).sum() + (x * dres).sum()      # noqa: E731
+    r = rr.prenorm(x, w, 1e-3, torch.float64)[1][0]
+    (dX, _), (dw, _) = rr.prenorm_bwd(dN, x, w, r, dres, torch.float64)
+    close(dX, differences(f, x))
+    if gain:
+        close(dw, differences(f, w))
+
+
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("use_next", [True, False])
+@pytest.mark.parametrize("use_dxo", [True, False])
+def test_join_gradients_are_the_forward_forms_slopes(post, use_next, use_dxo):
+    if not use_next and not use_dxo:
+        return
+    g = torch.Generator().manual_seed(2)
+    T, d, a, b, eps = 3, 8, 0.75, -0.5, 1e-3
+    X, Y, dXo, dN = (torch.randn(T, d, generator=g, dtype=F64) for _ in range(4))
+    wp, wn = torch.randn(d, generator=g, dtype=F64), torch.randn(d, generator=g, dtype=F64)
+    gate = torch.rand(T, generator=g, dtype=F64)
+    fwd = lambda: rr.join(X, Y, wp, gate, wn, eps, a, b, post, torch.float64)                       # noqa: E731
+
+    def f():
+        o = fwd()
+        return (o["Xo"][0] * dXo).sum() * use_dxo + (o["N"][0] * dN).sum() * use_next
+
+    o = fwd()
+    grad = rr.join_bwd(dXo if use_dxo else None, dN if use_next else None, Y, o["Xo"][0], wp, gate, wn,
+                       o["rstd_y"][0] if post else None, o["rstd_o"][0], a, b, post, torch.float64)
+    for name, x in (("dX", X), ("dY", Y), ("dw_post", wp), ("dgate", gate)) + ((("dw_next", wn),) if use_next else ()):
+        close(grad[name][0], differences(f, x))
+
+
+def test_unsort_gradients_are_the_forward_forms_slopes():
+    g = torch.Generator().manual_seed(3)
+    ids = torch.tensor([[0, 2], [2, 2], [-1, 1], [3, 0]])
+    n = 9
+    pos = torch.tensor(rr.plan(ids, 3, 1, 0, n)[4])
+    O, w, dY = (torch.randn(*s, generator=g, dtype=F64) for s in ((n, 8), (4, 2), (4, 8)))
+    f = lambda: (rr.unsort(O, w, pos, F64)[0] * dY).sum()                                          # noqa: E731
+    (dO, _), (dw, _) = rr.unsort_bwd(dY, O, w, pos, n, F64)
+    close(torch.nan_to_num(dO), differences(f, O))
+    close(dw, differences(f, w))
+    X = torch.randn(4, 8, generator=g, dtype=F64)
+    dXs = torch.randn(n, 8, generator=g, dtype=F64)
+    spread = lambda: sum(float((X[t] * dXs[pos[t, j]]).sum()) for t in range(4) for j in range(2) if pos[t, j] >= 0)   # noqa: E731
+    close(rr.unsort(dXs, None, pos, F64)[0], differences(spread, X))
+
+
+def test_plan_by_hand():
+    ids = torch.tensor([[1, 0], [1, 5], [0, 1], [-1, 1]])
+    assert rr.plan(ids, 2, 1, 0, 8) == ([2, 4], [0, 2, 6], [6, 0, 2, 0], [0, 2, 0, 1, 2, 3, -1, -1], [[2, 0], [3, -1], [1, 4], [-1, 5]])
+    assert rr.plan(ids, 2, 4, 0, 14)[1:3] == ([0, 4, 8], [6, 0, 2, 0])
+    counts, offsets, totals, _, pos = rr.plan(ids, 2, 128, 3, 256)
+    assert (counts, offsets, totals, pos[3]) == ([2, 3], [0, 128, 256], [5, 1, 2, 0], [-1, -1])
+
+
+# ---- refusals: status codes before any launch (there is no GPU here: a launch would fail with another status) -----
+
+
+def sort_cfg(**kw):
+    return etr.make_sort_config(**dict(dict(T=4, k=2, E=3, d=16, dtype=etr.BF16), **kw))
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(), etr.OK), (dict(T=0), etr.OK), (dict(T=-1), etr.ERR_ARG), (dict(k=0), etr.ERR_ARG), (dict(k=33), etr.ERR_SHAPE),
+    (dict(k=32), etr.OK), (dict(E=0), etr.ERR_ARG), (dict(E=1024), etr.OK), (dict(E=1025), etr.ERR_SHAPE), (dict(d=12), etr.ERR_SHAPE),
+    (dict(d=0), etr.ERR_ARG), (dict(dtype=2), etr.ERR_ARG), (dict(align=0), etr.ERR_ARG), (dict(align=1025), etr.ERR_SHAPE),
+    (dict(capacity=-1), etr.ERR_ARG), (dict(capacity=5), etr.ERR_SHAPE), (dict(capacity=5, align=128), etr.OK),
+    (dict(T=1 << 30), etr.ERR_SHAPE), (dict(E=1024, capacity=1 << 21, align=128), etr.ERR_SHAPE)])
+def test_sort_configurations(change, code):
+    cfg = sort_cfg(**change)
+    assert etr.sort_validate(cfg) == code
+    if code != etr.OK:
+        assert etr.sort_n_rows(cfg) == 0
+        n = C.c_size_t(0)
+        assert etr.lib().etr_sort_plan_bind(C.byref(cfg), None, C.c_size_t(0), None, C.byref(n)) == code
+        plan = etr.SortPlan(*[1 << 20] * 5)
+        assert etr.lib().etr_sort(C.addressof(cfg), 1 << 20, C.addressof(plan), None) == code
+
+
+def test_sort_rows_of_the_buffers():
+    assert etr.sort_n_rows(sort_cfg()) == 8
+    assert etr.sort_n_rows(sort_cfg(align=16)) == 8 + 3 * 15
+    assert etr.sort_n_rows(sort_cfg(T=1, E=100, align=16)) == 2 + 2 * 15
+    assert etr.sort_n_rows(sort_cfg(capacity=129, align=128)) == 3 * 256
+    assert etr.sort_n_rows(sort_cfg(T=0)) == 0
+
+
+def test_sort_pointers_are_checked():
+    L, cfg, ok = etr.lib(), sort_cfg(), 1 << 20
+    a = C.addressof(cfg)
+
+    def plan(**kw):
+        p = etr.SortPlan(*[ok] * 5)
+        for n, v in kw.items():
+            setattr(p, n, v)
+        return p
+
+    for name in ("counts", "offsets", "totals", "row_token", "pos"):
+        for value, code in ((None, etr.ERR_ARG), (ok + 4, etr.ERR_ALIGN)):
+            p = plan(**{name: value})
+            q = C.addressof(p)
+            assert L.etr_sort(a, ok, q, None) == code
+            assert L.etr_sort_rows(a, ok, q, ok, None) == code
+            assert L.etr_sort_rows_bwd(a, ok, q, ok, None) == code
+            assert L.etr_unsort_rows(a, ok, ok, q, ok, None) == code
+            assert L.etr_unsort_rows_bwd(a, ok, ok, ok, q, ok, ok, None) == code
+    p = plan()
+    q = C.addressof(p)
+    for bad, code in ((None, etr.ERR_ARG), (ok + 8, etr.ERR_ALIGN)):
+        assert L.etr_sort(a, bad, q, None) == code
+        for call, n in ((lambda v: L.etr_sort_rows(a, v[0], q, v[1], None), 2), (lambda v: L.etr_sort_rows_bwd(a, v[0], q, v[1], None), 2),
+                        (lambda v: L.etr_unsort_rows(a, v[0], v[1], q, v[2], None), 3),
+                        (lambda v: L.etr_unsort_rows_bwd(a, v[0], v[1], v[2], q, v[3], v[4], None), 5)):
+            for i in range(n):
+                assert call([bad if j == i else ok for j in range(n)]) == code
+    assert L.etr_sort(None, ok, q, None) == etr.ERR_ARG and L.etr_sort(a, ok, None, None) == etr.ERR_ARG
+    n, out = C.c_size_t(0), etr.SortPlan()
+    assert L.etr_sort_plan_bind(a, None, C.c_size_t(0), None, C.byref(n)) == etr.OK and n.value % 256 == 0
+    assert L.etr_sort_plan_bind(a, C.c_void_p(ok + 16), n, C.byref(out), None) == etr.ERR_ALIGN
+    assert L.etr_sort_plan_bind(a, C.c_void_p(ok), C.c_size_t(n.value - 1), C.byref(out), None) == etr.ERR_WORKSPACE
+    assert L.etr_sort_plan_bind(a, C.c_void_p(ok), n, C.byref(out), None) == etr.OK and out.counts == ok
+
+
+def norm_cfg(**kw):
+    return etr.make_norm_config(**dict(dict(T=4, d=16, dtype=etr.BF16, post_norm=True), **kw))
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(), etr.OK), (dict(T=0), etr.OK), (dict(T=-1), etr.ERR_ARG), (dict(d=0), etr.ERR_ARG), (dict(d=20), etr.ERR_SHAPE),
+    (dict(d=16384), etr.OK), (dict(d=16392), etr.ERR_SHAPE), (dict(dtype=7), etr.ERR_ARG), (dict(eps=0.0), etr.ERR_ARG),
+    (dict(eps=float("nan")), etr.ERR_ARG), (dict(eps=float("inf")), etr.ERR_ARG), (dict(eps=-1e-6), etr.ERR_ARG),
+    (dict(res_scale=float("nan")), etr.ERR_ARG), (dict(branch_scale=float("inf")), etr.ERR_ARG)])
+def test_norm_configurations(change, code):
+    cfg = norm_cfg(**change)
+    assert etr.norm_validate(cfg) == code
+    if code != etr.OK:
+        n, p = C.c_size_t(0), 1 << 20
+        assert etr.lib().etr_norm_workspace_bytes(C.byref(cfg), C.byref(n)) == code
+        assert etr.lib().etr_prenorm(C.addressof(cfg), p, p, p, p, None) == code
+        assert etr.lib().etr_join_bwd(C.addressof(cfg), *[p] * 15, None) == code
+
+
+def test_norm_pointers_are_checked():
+    L, cfg, ok = etr.lib(), norm_cfg(), 1 << 20
+    a = C.addressof(cfg)
+    calls = {"etr_prenorm": ("X", "w?", "N", "rstd?"),
+             "etr_join": ("X", "Y", "w_post?", "gate?", "w_next?", "Xo", "N?", "rstd_y?", "rstd_o?"),
+             "etr_prenorm_bwd": ("dN", "X", "w?", "rstd", "dres?", "dX", "dw?", "ws"),
+             "etr_join_bwd": ("dXo?", "dN?", "Y", "Xo", "w_post?", "gate?", "w_next?", "rstd_y", "rstd_o", "dX", "dY", "dw_post?",
+                              "dgate?", "dw_next?", "ws")}
+    for name, args in calls.items():
+        f = getattr(L, name)
+        for i, arg in enumerate(args):
+            assert f(a, *[ok + 4 if j == i else ok for j in range(len(args))], None) == etr.ERR_ALIGN, (name, arg)
+            if not arg.endswith("?"):
+                assert f(a, *[None if j == i else ok for j in range(len(args))], None) == etr.ERR_ARG, (name, arg)
+    j = dict(dXo=None, dN=None, Y=ok, Xo=None, w_post=None, gate=None, w_next=None, rstd_y=ok, rstd_o=None, dX=ok, dY=ok,
+             dw_post=None, dgate=None, dw_next=None, ws=None)
+    assert L.etr_join_bwd(a, *j.values(), None) == etr.ERR_ARG                     # neither gradient
+    assert L.etr_join_bwd(a, *dict(j, dXo=ok, dw_next=ok, ws=ok).values(), None) == etr.ERR_ARG   # dw_next without dN
+    assert L.etr_join_bwd(a, *dict(j, dXo=ok, dw_post=ok).values(), None) == etr.ERR_ARG      # a gain's gradient without ws
+
+
+def test_binding_refuses_what_addresses_do_not_show():
+    """Tensors of the wrong type, size or place never reach the library."""
+    cfg = norm_cfg()
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    with pytest.raises(etr.EtrError):
+        etr.prenorm(cfg, x, None, x.clone())                       # on the CPU
+    dev = torch.device("cpu")
+    for t, n, code in ((x.float(), 64, etr.ERR_ARG), (x, 63, etr.ERR_SHAPE), (x.t(), 64, etr.ERR_SHAPE), (None, 64, etr.ERR_ARG)):
+        with pytest.raises(etr.EtrError) as e:
+            etr._arg("call", t, torch.bfloat16, n, dev)
+        assert e.value.code == code
+    assert etr._arg("call", x, torch.bfloat16, 64, dev) == x.data_ptr()
+    with pytest.raises(etr.EtrError) as e:
+        etr._norm_ws("call", cfg, torch.empty(16, dtype=torch.uint8), dev)
+    assert e.value.code == etr.ERR_WORKSPACE
