@@ -450,6 +450,7 @@ typedef struct etr_sort_plan {
   int32_t* totals;            /* [4]    pairs with a row, pairs dropped, pairs without an expert, 0 */
   int32_t* row_token;         /* [etr_sort_n_rows] token of each row, -1 where there is none */
   int32_t* pos;               /* [T,k]  row of each pair, -1 where there is none */
+  int32_t* scratch;           /* [18 E] of etr_sort's own */
 } etr_sort_plan;
 
 etr_status etr_sort_validate(const etr_sort_config* cfg);
@@ -457,7 +458,7 @@ etr_status etr_sort_validate(const etr_sort_config* cfg);
 int64_t etr_sort_n_rows(const etr_sort_config* cfg);
 /* Size of a block for the plan (need, may be NULL) and its carving (out, may be NULL; base 256-byte aligned). */
 etr_status etr_sort_plan_bind(const etr_sort_config* cfg, void* base, size_t bytes, etr_sort_plan* out, size_t* need);
-/* topk_idx [T,k] int32.  Fills every member of the plan.  One launch. */
+/* topk_idx [T,k] int32.  Fills every member of the plan.  One launch, two where T*k > 8192. */
 etr_status etr_sort(const etr_sort_config* cfg, const int32_t* topk_idx, const etr_sort_plan* plan, void* stream);
 /* Xs[pos[t][j],:] = X[t,:]; pad rows 0. */
 etr_status etr_sort_rows(const etr_sort_config* cfg, const void* X, const etr_sort_plan* plan, void* Xs, void* stream);

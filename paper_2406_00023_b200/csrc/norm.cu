@@ -19,57 +19,33 @@ struct NormArgs {
   float eps, a, b;
 };
 
-// Sum over a group of TPR threads (a row), in every thread of it.  Two arrays take turns from sum to sum, so that one barrier
-// a sum is enough: whoever writes an array again has passed the barrier of the sum between, and so has every reader.
-template <int TPR, int BLOCK>
+// How rows lie on a block's threads: tpr threads hold a row (a power of two up to 32, or whole warps), NV pieces of 16 bytes each
+// (piece u of a thread is piece tg + u tpr of the row), rpb rows side by side in a block.
+struct RowShape { int tpr, rpb, stages; };
+
+// Sum over a row's threads, in every one of them.  Two arrays take turns from sum to sum, so that one barrier a sum is
+// enough: whoever writes an array again has passed the barrier of the sum between, and so has every reader.
+constexpr int NORM_MAX_WARPS = 16;                // 512 threads
 struct RowSum {
-  float (*red)[BLOCK / 32];
-  int turn;
+  float (*red)[NORM_MAX_WARPS];                   // [2][NORM_MAX_WARPS]
+  int tpr, turn;
   __device__ __forceinline__ float operator()(float v) {
+    if (tpr <= 32) {
+      for (int o = tpr >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      return v;
+    }
     v = warp_sum(v);
-    if (TPR <= 32) return v;
-    const int warp = threadIdx.x >> 5, first = warp / (TPR / 32) * (TPR / 32);
+    const int warp = threadIdx.x >> 5, wpr = tpr >> 5, first = warp / wpr * wpr;
     if ((threadIdx.x & 31) == 0) red[turn][warp] = v;
     __syncthreads();
     v = 0.f;
-#pragma unroll
-    for (int w = 0; w < TPR / 32; ++w) v += red[turn][first + w];
+#pragma unroll 4
+    for (int w = 0; w < wpr; ++w) v += red[turn][first + w];
     turn ^= 1;
     return v;
   }
 };
 
-// A row is held by TPR threads, NV pieces of 16 bytes each: piece u of a thread is piece tg + u TPR of the row.
-template <class T> constexpr int PIECE = 16 / (int)sizeof(T);             // values in a piece
-template <int TPR> constexpr int NORM_BLOCK = TPR > 256 ? TPR : 256;
-
-template <class T>
-__device__ __forceinline__ void unpack(const uint4 q, float* v) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (sizeof(T) == 4) {
-      v[i] = __uint_as_float(w[i]);
-    } else {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-}
-template <class T>
-__device__ __forceinline__ uint4 pack(const float* v) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (sizeof(T) == 4) {
-      w[i] = __float_as_uint(v[i]);
-    } else {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 template <int N>
 __device__ __forceinline__ void load_gain(const float* w, int col, float* out) {       // w == nullptr: ones
 #pragma unroll
@@ -79,44 +55,37 @@ __device__ __forceinline__ void load_gain(const float* w, int col, float* out) {
   }
 }
 
-// The rows of up to NT tensors, S tiles ahead.  A thread copies (cp.async) exactly the pieces that it reads itself, so that a
-// wait for its own copies is all the synchronisation the ring needs.  S = 0: no ring, read from global memory (rows so
-// long that two tiles do not fit).
-template <int S, int NT, int BLOCK, int NV>
+// The rows of up to NT tensors, tiles ahead of their use.  A thread copies (cp.async) exactly the pieces that it reads
+// itself, so that a wait for its own copies is all the synchronisation the ring needs.
+template <int NT, int NV>
 struct RowRing {
   uint4* smem;
-  __device__ __forceinline__ uint4* slot(int stage, int tensor, int u) const { return smem + ((stage * NT + tensor) * NV + u) * BLOCK + threadIdx.x; }
+  __device__ __forceinline__ uint4* slot(int stage, int tensor, int u) const { return smem + ((stage * NT + tensor) * NV + u) * blockDim.x + threadIdx.x; }
   __device__ __forceinline__ void fetch(int stage, int tensor, int u, const uint4* src) const {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot(stage, tensor, u))), "l"(src) : "memory");
   }
   __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
-  __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group %0;" ::"n"(S > 0 ? S - 1 : 0) : "memory"); }
+  // all copies but those of the stages - 1 youngest tiles have arrived
+  __device__ __forceinline__ void wait(int stages) const {
+    if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;" ::: "memory");
+  }
 };
 
-// Stages of a ring whose tile takes `bytes`, with `ctas` CTAs of 200 KiB between them on an SM; fewer than two: none.
-constexpr int ring_stages(int bytes, int ctas, int most) {
-  return 200 * 1024 / ctas / bytes < 2 ? 0 : 200 * 1024 / ctas / bytes < most ? 200 * 1024 / ctas / bytes : most;
-}
-
-template <class T, int TPR, int NV, bool JOIN>
-struct FwdShape {
-  static constexpr int BLOCK = NORM_BLOCK<TPR>, RPB = BLOCK / TPR, NT = JOIN ? 2 : 1;
-  static constexpr int CTAS = 768 / BLOCK;
-  static constexpr int TILE = NT * BLOCK * NV * 16;
-  static constexpr int S = ring_stages(TILE, CTAS, 4), SMEM = S * TILE;
-};
+// Forward: at most 80 registers a thread, so that 768 threads fit an SM; backward: 128 and 512.
+constexpr int NORM_FWD_REGS = 80, NORM_FWD_THREADS = 768, NORM_BWD_REGS = 128, NORM_BWD_THREADS = 512;
 
 // Forward.  JOIN false: prenorm of X.  Blocks walk tiles of RPB rows in strides, with the gains in registers.
-template <class T, int TPR, int NV, bool JOIN>
-__global__ void __launch_bounds__(NORM_BLOCK<TPR>, FwdShape<T, TPR, NV, JOIN>::CTAS)
-norm_fwd_kernel(const NormArgs p) {
-  using Sh = FwdShape<T, TPR, NV, JOIN>;
-  constexpr int BLOCK = Sh::BLOCK, RPB = Sh::RPB, S = Sh::S, P = PIECE<T>;
+template <class T, int NV, bool RING, bool JOIN>
+__global__ void __maxnreg__(NV > 2 ? 128 : NORM_FWD_REGS)
+norm_fwd_kernel(const NormArgs p, const RowShape sh) {
+  constexpr int P = PIECE<T>, NT = JOIN ? 2 : 1;
   extern __shared__ uint4 ring_smem[];
-  __shared__ float red[2][BLOCK / 32];
-  RowSum<TPR, BLOCK> row_sum{red, 0};
-  const RowRing<S, Sh::NT, BLOCK, NV> ring{ring_smem};
-  const int tg = threadIdx.x % TPR, row = threadIdx.x / TPR, np = p.d / P;
+  __shared__ float red[2][NORM_MAX_WARPS];
+  RowSum row_sum{red, sh.tpr, 0};
+  const RowRing<NT, NV> ring{ring_smem};
+  const int TPR = sh.tpr, RPB = sh.rpb, S = sh.stages;
+  const int row = threadIdx.x / TPR, tg = threadIdx.x - row * TPR, np = p.d / P;
   const float inv_d = 1.f / (float)p.d;
   const long long step = (long long)gridDim.x * RPB;
   auto fetch = [&](int stage, long long t) {
@@ -126,7 +95,7 @@ norm_fwd_kernel(const NormArgs p) {
       for (int u = 0; u < NV; ++u) {
         const int g = tg + u * TPR;
         if (g >= np) continue;
-        if (JOIN) ring.fetch(stage, Sh::NT - 1, u, (const uint4*)p.Y + off + g);
+        if (JOIN) ring.fetch(stage, NT - 1, u, (const uint4*)p.Y + off + g);
         ring.fetch(stage, 0, u, (const uint4*)p.X + off + g);
       }
     }
@@ -134,7 +103,8 @@ norm_fwd_kernel(const NormArgs p) {
   };
   grid_sync();
   long long t = (long long)blockIdx.x * RPB + row;
-  for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
+  if (RING)
+    for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
   float wp[JOIN ? NV : 1][P], wn[NV][P];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -147,14 +117,14 @@ norm_fwd_kernel(const NormArgs p) {
   for (long long tb = (long long)blockIdx.x * RPB; tb < p.T; tb += step, t += step) {
     const bool live = t < p.T;
     const size_t off = (size_t)(live ? t : 0) * np;
-    if (S > 0) {
+    if (RING) {
       fetch(stage == 0 ? S - 1 : stage - 1, t + (S - 1) * step);
-      ring.wait();
+      ring.wait(S);
     }
     auto piece = [&](int tensor, const void* base, int u) {
       const int g = tg + u * TPR;
       if (!live || g >= np) return make_uint4(0, 0, 0, 0);
-      return S > 0 ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
+      return RING ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
     };
     float x[NV][P];
 #pragma unroll
@@ -162,7 +132,7 @@ norm_fwd_kernel(const NormArgs p) {
     if (JOIN) {
       float y[NV][P], f = p.b * gate;
 #pragma unroll
-      for (int u = 0; u < NV; ++u) unpack<T>(piece(Sh::NT - 1, p.Y, u), y[u]);
+      for (int u = 0; u < NV; ++u) unpack<T>(piece(NT - 1, p.Y, u), y[u]);
       if (p.gate && t + step < p.T) gate = p.gate[t + step];
       if (p.post) {
         float s = 0.f;
@@ -199,32 +169,23 @@ norm_fwd_kernel(const NormArgs p) {
         ((uint4*)p.N)[off + g] = pack<T>(x[u]);
       }
     }
-    stage = S > 0 && stage + 1 < S ? stage + 1 : 0;
+    stage = stage + 1 < S ? stage + 1 : 0;
   }
 }
-
-template <class T, int TPR, int NV, bool JOIN>
-struct BwdShape {
-  static constexpr int BLOCK = NORM_BLOCK<TPR>, RPB = BLOCK / TPR, NT = JOIN ? 4 : 3;
-  static constexpr int CTAS = 512 / BLOCK;
-  static constexpr int TILE = NT * BLOCK * NV * 16;
-  static constexpr int S = ring_stages(TILE, CTAS, 3), SMEM = S * TILE;
-  static constexpr int FOLD = RPB > 1 ? BLOCK * NV * PIECE<T> * 4 : 0;       // one row of partial sums per row group
-};
 
 // Backward.  Blocks walk tiles of RPB rows in strides, a thread always on the same columns, so the gains' gradients add up in
 // registers; a block leaves one row of partial sums per gain, which norm_dw_kernel adds in order.
 // JOIN false: prenorm (Xo_in is its input X, dXo the gradient that comes along the residual, may be NULL; no y).
-template <class T, int TPR, int NV, bool JOIN>
-__global__ void __launch_bounds__(NORM_BLOCK<TPR>, BwdShape<T, TPR, NV, JOIN>::CTAS)
-norm_bwd_kernel(const NormArgs p) {
-  using Sh = BwdShape<T, TPR, NV, JOIN>;
-  constexpr int BLOCK = Sh::BLOCK, RPB = Sh::RPB, S = Sh::S, P = PIECE<T>;
+template <class T, int NV, bool RING, bool JOIN>
+__global__ void __maxnreg__(NORM_BWD_REGS)
+norm_bwd_kernel(const NormArgs p, const RowShape sh) {
+  constexpr int P = PIECE<T>, NT = JOIN ? 4 : 3;
   extern __shared__ uint4 ring_smem[];
-  __shared__ float red[2][BLOCK / 32];
-  RowSum<TPR, BLOCK> row_sum{red, 0};
-  const RowRing<S, Sh::NT, BLOCK, NV> ring{ring_smem};
-  const int tg = threadIdx.x % TPR, row = threadIdx.x / TPR, np = p.d / P;
+  __shared__ float red[2][NORM_MAX_WARPS];
+  RowSum row_sum{red, sh.tpr, 0};
+  const RowRing<NT, NV> ring{ring_smem};
+  const int TPR = sh.tpr, RPB = sh.rpb, S = sh.stages;
+  const int row = threadIdx.x / TPR, tg = threadIdx.x - row * TPR, np = p.d / P;
   const float inv_d = 1.f / (float)p.d;
   const long long step = (long long)gridDim.x * RPB;
   enum { DN, XO, DXO, YY };
@@ -247,7 +208,8 @@ norm_bwd_kernel(const NormArgs p) {
   };
   grid_sync();
   long long t = (long long)blockIdx.x * RPB + row;
-  for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
+  if (RING)
+    for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
   float wp[JOIN ? NV : 1][P], wn[NV][P], acc_p[JOIN ? NV : 1][P], acc_n[NV][P];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -275,14 +237,14 @@ norm_bwd_kernel(const NormArgs p) {
     const size_t off = (size_t)(live ? t : 0) * np;
     const float ro = r_o, ry = r_y, ga = gate;
     scalars(t + step);
-    if (S > 0) {
+    if (RING) {
       fetch(stage == 0 ? S - 1 : stage - 1, t + (S - 1) * step);
-      ring.wait();
+      ring.wait(S);
     }
     auto piece = [&](int tensor, const void* base, int u) {
       const int g = tg + u * TPR;
       if (base == nullptr || !live || g >= np) return make_uint4(0, 0, 0, 0);
-      return S > 0 ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
+      return RING ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
     };
     float G[NV][P];
 #pragma unroll
@@ -347,7 +309,7 @@ norm_bwd_kernel(const NormArgs p) {
         ((uint4*)p.dY)[off + g] = pack<T>(y);
       }
     }
-    stage = S > 0 && stage + 1 < S ? stage + 1 : 0;
+    stage = stage + 1 < S ? stage + 1 : 0;
   }
   // One row of partial sums per block and gain; where a block has several row groups they are added first, through the
   // ring's memory (every copy into it has arrived: the last groups waited for are empty).
@@ -370,7 +332,7 @@ norm_bwd_kernel(const NormArgs p) {
     }
     if (RPB > 1) {
       __syncthreads();
-      for (int c = threadIdx.x; c < p.d; c += BLOCK) {
+      for (int c = threadIdx.x; c < p.d; c += blockDim.x) {
         float s = 0.f;
         for (int q = 0; q < RPB; ++q) s += fold[(size_t)q * p.d + c];
         part[(size_t)blockIdx.x * p.d + c] = s;
@@ -420,69 +382,95 @@ static etr_status norm_ptrs(std::initializer_list<const void*> need, std::initia
   return ETR_OK;
 }
 
-// Threads per row: as few as hold it with 2 pieces of 16 bytes each, at least a warp, at most 512 (then 4 or 8 pieces).
-static int norm_pieces(const NormArgs& p, int dtype) { return p.d * (int)elem_bytes(dtype) / 16; }
-static int norm_tpr(int pieces) {
-  int tpr = 32;
-  while (tpr < 512 && pieces > 2 * tpr) tpr *= 2;
-  return tpr;
+// Rows on threads.  2 pieces a thread where that is whole warps (one piece for rows within a warp), 4 or 8 where 512 threads
+// would not hold the row; about 256 threads a block.
+static int norm_pieces(int d, int dtype) { return d * (int)elem_bytes(dtype) / 16; }
+static int norm_nv(int pieces) { return pieces <= 32 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8; }
+static RowShape norm_shape(int pieces) {
+  const int nv = norm_nv(pieces);
+  RowShape s = {4, 1, 0};
+  if (nv == 1)
+    while (s.tpr < pieces) s.tpr *= 2;
+  else
+    s.tpr = ceil_div(pieces, 32 * nv) * 32;
+  s.rpb = s.tpr < 256 ? 256 / s.tpr : 1;
+  return s;
 }
 
-template <template <class, int, int> class K, class T>
+template <template <class, int> class K, class T>
 static etr_status norm_by_shape(const NormArgs& p, cudaStream_t st) {
-  const int pieces = p.d / PIECE<T>, tpr = norm_tpr(pieces);
-  switch (tpr) {
-    case 32: return pieces <= 32 ? K<T, 32, 1>::run(p, st) : K<T, 32, 2>::run(p, st);
-    case 64: return K<T, 64, 2>::run(p, st);
-    case 128: return K<T, 128, 2>::run(p, st);
-    case 256: return K<T, 256, 2>::run(p, st);
+  const int pieces = p.d / PIECE<T>;
+  const RowShape s = norm_shape(pieces);
+  switch (norm_nv(pieces)) {
+    case 1: return K<T, 1>::run(p, s, st);
+    case 2: return K<T, 2>::run(p, s, st);
+    case 4: return K<T, 4>::run(p, s, st);
   }
-  if (pieces <= 1024) return K<T, 512, 2>::run(p, st);
-  if (sizeof(T) == 2 || pieces <= 2048) return K<T, 512, 4>::run(p, st);
-  return K<T, 512, sizeof(T) == 2 ? 4 : 8>::run(p, st);
+  return K<T, sizeof(T) == 2 ? 4 : 8>::run(p, s, st);      // 8: fp32 rows only
 }
-template <template <class, int, int> class K>
+template <template <class, int> class K>
 static etr_status norm_by_type(int dtype, const NormArgs& p, cudaStream_t st) {
   return dtype == ETR_BF16 ? norm_by_shape<K, __nv_bfloat16>(p, st) : norm_by_shape<K, float>(p, st);
 }
 
-template <class Sh, class K>
-static etr_status norm_launch(const char* name, K kernel, int smem, long long ctas, const NormArgs& p, cudaStream_t st) {
-  static std::atomic<unsigned long long> done{0};
-  if (smem > 0 && !ensure_dyn_smem(kernel, (size_t)smem, done)) return ETR_ERR_CUDA;
-  const long long tiles = ((long long)p.T + Sh::RPB - 1) / Sh::RPB;
+// A ring of three tiles, or two, within the CTA's part of 200 KiB; 0: rows so long that two tiles do not fit are read without
+// a ring.
+static int ring_stages(long long tile, int ctas) {
+  const long long n = 200 * 1024 / ctas / tile;
+  return n < 2 ? 0 : n < 3 ? 2 : 3;
+}
+
+template <class K>
+static etr_status norm_launch(const char* name, K kernel, std::atomic<unsigned long long>& done, size_t smem, int ctas, const NormArgs& p,
+                              const RowShape& s, cudaStream_t st) {
+  if (!ensure_dyn_smem(kernel, 200 * 1024, done)) return ETR_ERR_CUDA;
+  const long long tiles = ((long long)p.T + s.rpb - 1) / s.rpb, most = (long long)current_sm_count() * ctas;
   ETR_TIME_BEGIN(name);
-  launch_kernel(kernel, (unsigned)(tiles < ctas ? tiles : ctas), Sh::BLOCK, (size_t)smem, st, 1, p);
+  launch_kernel(kernel, (unsigned)(tiles < most ? tiles : most), s.tpr * s.rpb, smem, st, 1, p, s);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
 }
 
-template <class T, int TPR, int NV>
+template <class T, int NV>
 struct FwdRun {
   template <bool JOIN>
-  static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
-    using Sh = FwdShape<T, TPR, NV, JOIN>;
-    return norm_launch<Sh>(name, norm_fwd_kernel<T, TPR, NV, JOIN>, Sh::SMEM, (long long)current_sm_count() * Sh::CTAS, p, st);
+  static etr_status go(const char* name, const NormArgs& p, RowShape s, cudaStream_t st) {
+    static std::atomic<unsigned long long> done{0}, done0{0};
+    const int block = s.tpr * s.rpb, threads = NV > 2 ? 512 : NORM_FWD_THREADS, ctas = threads / block > 1 ? threads / block : 1;
+    const long long tile = (JOIN ? 2ll : 1ll) * NV * block * 16;
+    s.stages = ring_stages(tile, ctas);
+    if (NV > 2 && s.stages == 0) return norm_launch(name, norm_fwd_kernel<T, NV, NV <= 2, JOIN>, done0, 0, ctas, p, s, st);
+    return norm_launch(name, norm_fwd_kernel<T, NV, true, JOIN>, done, (size_t)(s.stages * tile), ctas, p, s, st);
   }
-  static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_kernel", p, st) : go<false>("prenorm_kernel", p, st); }
+  static etr_status run(const NormArgs& p, const RowShape& s, cudaStream_t st) {
+    return p.Y ? go<true>("join_kernel", p, s, st) : go<false>("prenorm_kernel", p, s, st);
+  }
 };
 
-// Blocks of the backward kernels: 512 threads on every SM.
-static int norm_bwd_blocks(const NormArgs& p, int dtype) {
-  const int tpr = norm_tpr(norm_pieces(p, dtype)), block = tpr > 256 ? tpr : 256, rpb = block / tpr;
-  const long long want = ((long long)p.T + rpb - 1) / rpb, cap = (long long)current_sm_count() * (512 / block);
-  return (int)(want < cap ? want : cap);
+static int norm_bwd_ctas(const RowShape& s) { return NORM_BWD_THREADS / (s.tpr * s.rpb) > 1 ? NORM_BWD_THREADS / (s.tpr * s.rpb) : 1; }
+// Blocks of the backward kernels, each of which leaves a row of partial sums per gain; at most NORM_BWD_MOST an SM.
+constexpr int NORM_BWD_MOST = 3;                  // blocks of 160 threads
+static int norm_bwd_blocks(int T, int d, int dtype) {
+  const RowShape s = norm_shape(norm_pieces(d, dtype));
+  const long long want = ((long long)T + s.rpb - 1) / s.rpb, most = (long long)current_sm_count() * norm_bwd_ctas(s);
+  return (int)(want < most ? want : most);
 }
 
-template <class T, int TPR, int NV>
+template <class T, int NV>
 struct BwdRun {
   template <bool JOIN>
-  static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
-    using Sh = BwdShape<T, TPR, NV, JOIN>;
-    return norm_launch<Sh>(name, norm_bwd_kernel<T, TPR, NV, JOIN>, Sh::SMEM > Sh::FOLD ? Sh::SMEM : Sh::FOLD,
-                           (long long)current_sm_count() * Sh::CTAS, p, st);
+  static etr_status go(const char* name, const NormArgs& p, RowShape s, cudaStream_t st) {
+    static std::atomic<unsigned long long> done{0}, done0{0};
+    const int block = s.tpr * s.rpb, ctas = norm_bwd_ctas(s);
+    const long long tile = (JOIN ? 4ll : 3ll) * NV * block * 16, fold = s.rpb > 1 ? (long long)s.rpb * p.d * 4 : 0;
+    s.stages = ring_stages(tile, ctas);
+    if (NV > 2 && s.stages == 0) return norm_launch(name, norm_bwd_kernel<T, NV, NV <= 2, JOIN>, done0, (size_t)fold, ctas, p, s, st);
+    const long long smem = s.stages * tile;
+    return norm_launch(name, norm_bwd_kernel<T, NV, true, JOIN>, done, (size_t)(smem > fold ? smem : fold), ctas, p, s, st);
   }
-  static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_bwd_kernel", p, st) : go<false>("prenorm_bwd_kernel", p, st); }
+  static etr_status run(const NormArgs& p, const RowShape& s, cudaStream_t st) {
+    return p.Y ? go<true>("join_bwd_kernel", p, s, st) : go<false>("prenorm_bwd_kernel", p, s, st);
+  }
 };
 
 static etr_status norm_dw(const etr_norm_config* c, const NormArgs& p, float* dw_next, float* dw_post, cudaStream_t st) {
@@ -491,7 +479,7 @@ static etr_status norm_dw(const etr_norm_config* c, const NormArgs& p, float* dw
   const float* a = dw_next ? p.part_next : p.part_post;
   ETR_TIME_BEGIN("norm_dw_kernel");
   launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 256, 0, st, 1, a, (const float*)p.part_post, dw_next ? dw_next : dw_post,
-                dw_post, norm_bwd_blocks(p, c->dtype), c->d);
+                dw_post, norm_bwd_blocks(c->T, c->d, c->dtype), c->d);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
 }
@@ -514,7 +502,7 @@ etr_status etr_norm_validate(const etr_norm_config* c) { return norm_valid(c); }
 etr_status etr_norm_workspace_bytes(const etr_norm_config* c, size_t* bytes) {
   if (bytes == nullptr) return ETR_ERR_ARG;
   ETR_TRY(norm_valid(c));
-  *bytes = align_up((size_t)2 * current_sm_count() * 2 * c->d * 4, 256);
+  *bytes = align_up((size_t)2 * current_sm_count() * NORM_BWD_MOST * c->d * 4, 256);
   return ETR_OK;
 }
 
@@ -568,7 +556,7 @@ etr_status etr_join_bwd(const etr_norm_config* c, const void* dXo, const void* d
   p.dXo = dXo; p.dN = dN; p.Y = Y; p.Xo_in = Xo; p.w_post = w_post; p.gate = gate; p.w_next = w_next; p.rstd_y = rstd_y; p.rstd_o = rstd_o;
   p.dX = dX; p.dY = dY; p.dgate = dgate;
   p.part_next = dw_next ? (float*)ws : nullptr;
-  p.part_post = dw_post ? (float*)ws + (size_t)current_sm_count() * 2 * c->d : nullptr;
+  p.part_post = dw_post ? (float*)ws + (size_t)current_sm_count() * NORM_BWD_MOST * c->d : nullptr;
   if (c->T > 0) ETR_TRY(norm_by_type<BwdRun>(c->dtype, p, (cudaStream_t)stream));
   return norm_dw(c, p, dw_next, dw_post, (cudaStream_t)stream);
 }

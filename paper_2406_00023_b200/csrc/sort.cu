@@ -2,55 +2,88 @@
 // the four row passes.  Stable: the rows of an expert hold its pairs in ascending (token, choice) order.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace etr {
 
-constexpr int SORT_WARPS = 16;
-constexpr int SORT_MAX_CLUSTER = 8;
-constexpr int SORT_MAX_E = 1024;
+constexpr int SORT_WARPS = 16;                   // at most
+constexpr int SORT_CLUSTER = 8;
+constexpr int SORT_MAX_CLUSTERS = 18;            // 144 of the 148 SMs
+constexpr int SORT_RUN = 64;                     // pairs per warp that are worth another CTA
 
 struct SortShape {
   int N, k, E, align, capacity, stride, n_rows;      // stride: rows between experts in the capacity form, else 0
+  int run;                                           // consecutive pairs per warp, whole rounds of 32
 };
 
-// The plan, by one cluster.  Every warp owns a run of consecutive pairs and counts its ids per expert (shared memory), the
-// warps' counts become prefix sums within the CTA and, through distributed shared memory, across the cluster; the row
-// of a pair is then its expert's start, plus the pairs of earlier warps, plus those before it in its own warp (one
-// match over the warp's 32 ids a round).  No atomics decide an order, so the plan is stable and the same every time.
+// Long batches, first of two launches: pairs per cluster and expert, part[cluster][E].  The same split over clusters as in
+// sort_plan_kernel.
 __global__ void __launch_bounds__(SORT_WARPS * 32)
-sort_plan_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
-                 int32_t* __restrict__ totals, int32_t* __restrict__ row_token, int32_t* __restrict__ pos) {
+sort_count_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ part) {
+  extern __shared__ int mine[];                  // [E]
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, threads = blockDim.x;
+  const int per = s.run * (threads >> 5);
+  const long long beg = (long long)blockIdx.x * per, end = min((long long)s.N, beg + per);
+  for (int e = tid; e < s.E; e += threads) mine[e] = 0;
+  __syncthreads();
+  grid_sync();
+#pragma unroll 4
+  for (long long i = beg + tid; i < end; i += threads) {
+    const int e = ids[i];
+    if ((unsigned)e < (unsigned)s.E) atomicAdd(&mine[e], 1);
+  }
+  cluster.sync();
+  for (int e = (int)cluster.block_rank() * threads + tid; e < s.E; e += SORT_CLUSTER * threads) {
+    int sum = 0;
+#pragma unroll
+    for (int c = 0; c < SORT_CLUSTER; ++c) sum += cluster.map_shared_rank(mine, c)[e];
+    part[(size_t)(blockIdx.x / SORT_CLUSTER) * s.E + e] = sum;
+  }
+  cluster.sync();
+}
+
+// The plan.  Every warp owns a run of consecutive pairs and counts its ids per expert (shared memory); the warps' counts become
+// prefix sums within the CTA, through distributed shared memory across the cluster, and through `part` across the
+// clusters (nclusters > 1).  The row of a pair is then its expert's start, plus the pairs of earlier warps, plus those
+// before it in its own warp (one match over the warp's 32 ids a round).  No atomics decide an order, so the plan is
+// stable and the same every time.  Bound by the latency of that chain: a short batch is one launch of one small CTA.
+__global__ void __launch_bounds__(SORT_WARPS * 32)
+sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclusters, int32_t* __restrict__ counts,
+                 int32_t* __restrict__ offsets, int32_t* __restrict__ totals, int32_t* __restrict__ row_token,
+                 int32_t* __restrict__ pos) {
   extern __shared__ int sm[];
-  int* wc = sm;                                  // [SORT_WARPS][E] pairs of this warp, then of the warps before it
-  int* mine = wc + SORT_WARPS * s.E;             // [E] pairs of this CTA
+  cg::cluster_group cluster = cg::this_cluster();
+  const int threads = blockDim.x, warps = threads >> 5, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int ncta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), my_cluster = blockIdx.x / ncta;
+  int* wc = sm;                                  // [warps][E] pairs of this warp, then of the warps before it
+  int* mine = wc + warps * s.E;                  // [E] pairs of this CTA
   int* start = mine + s.E;                       // [E] first row of the expert
   int* kept = start + s.E;                       // [E]
-  __shared__ int s_warp[SORT_WARPS], s_found[SORT_WARPS], s_kept[SORT_WARPS];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = (int)cluster.block_rank(), ncta = (int)cluster.num_blocks();
-  for (int i = tid; i < SORT_WARPS * s.E; i += SORT_WARPS * 32) wc[i] = 0;
-  grid_sync();
-  __syncthreads();
-  const int runs = ncta * SORT_WARPS;
-  const int run = ((s.N + runs - 1) / runs + 31) & ~31;            // pairs per warp, whole rounds of 32
-  const long long beg = (long long)(rank * SORT_WARPS + warp) * run;
-  const int n = (int)max(0ll, min((long long)run, (long long)s.N - beg));
+  __shared__ int s_rows[SORT_WARPS], s_found[SORT_WARPS], s_kept[SORT_WARPS];
+  for (int i = tid; i < warps * s.E; i += threads) wc[i] = 0;
+  const long long beg = ((long long)blockIdx.x * warps + warp) * s.run;
+  const int n = (int)max(0ll, min((long long)s.run, (long long)s.N - beg));
   int* cnt = wc + warp * s.E;
+  __syncthreads();
+  grid_sync();
+#pragma unroll 4
   for (int i = lane; i < n; i += 32) {
     const int e = ids[beg + i];
     if ((unsigned)e < (unsigned)s.E) atomicAdd(&cnt[e], 1);
   }
   __syncthreads();
-  for (int e = tid; e < s.E; e += SORT_WARPS * 32) {
+  for (int e = tid; e < s.E; e += threads) {
     int acc = 0;
-    for (int w = 0; w < SORT_WARPS; ++w) { const int c = wc[w * s.E + e]; wc[w * s.E + e] = acc; acc += c; }
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) { const int c = wc[w * s.E + e]; wc[w * s.E + e] = acc; acc += c; }
     mine[e] = acc;
   }
-  cluster.sync();
+  if (ncta > 1) cluster.sync(); else __syncthreads();
   // Experts [2 tid, 2 tid + 2): pairs found, kept, and rows taken; the starts by a scan over the CTA's threads.
   int rows[2] = {0, 0}, found = 0, keeps = 0;
 #pragma unroll
@@ -63,13 +96,23 @@ sort_plan_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ counts, 
       all += v;
       before += c < rank ? v : 0;
     }
+    if (nclusters > 1) {
+      all = 0;
+#pragma unroll 6
+      for (int c = 0; c < nclusters; ++c) {
+        const int v = part[(size_t)c * s.E + e];
+        all += v;
+        before += c < my_cluster ? v : 0;
+      }
+    }
     const int keep = s.capacity ? min(all, s.capacity) : all;
-    for (int w = 0; w < SORT_WARPS; ++w) wc[w * s.E + e] += before;
+    if (before)
+      for (int w = 0; w < warps; ++w) wc[w * s.E + e] += before;
     kept[e] = keep;
     found += all;
     keeps += keep;
     rows[u] = s.capacity ? s.stride : (keep + s.align - 1) / s.align * s.align;
-    if (rank == 0) counts[e] = keep;
+    if (blockIdx.x == 0) counts[e] = keep;
   }
   int inc = rows[0] + rows[1];
 #pragma unroll
@@ -82,13 +125,13 @@ sort_plan_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ counts, 
     found += __shfl_xor_sync(0xffffffffu, found, o);
     keeps += __shfl_xor_sync(0xffffffffu, keeps, o);
   }
-  if (lane == 31) { s_warp[warp] = inc; s_found[warp] = found; s_kept[warp] = keeps; }
+  if (lane == 31) { s_rows[warp] = inc; s_found[warp] = found; s_kept[warp] = keeps; }
   __syncthreads();
   int at = inc - rows[0] - rows[1], end = 0;
   found = keeps = 0;
-  for (int w = 0; w < SORT_WARPS; ++w) {
-    at += w < warp ? s_warp[w] : 0;
-    end += s_warp[w];
+  for (int w = 0; w < warps; ++w) {
+    at += w < warp ? s_rows[w] : 0;
+    end += s_rows[w];
     found += s_found[w];
     keeps += s_kept[w];
   }
@@ -97,38 +140,47 @@ sort_plan_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ counts, 
     const int e = 2 * tid + u;
     if (e < s.E) {
       start[e] = at;
-      if (rank == 0) offsets[e] = at;
+      if (blockIdx.x == 0) offsets[e] = at;
     }
     at += rows[u];
   }
-  if (rank == 0 && tid == 0) {
+  if (blockIdx.x == 0 && tid == 0) {
     offsets[s.E] = end;
     totals[0] = keeps; totals[1] = found - keeps; totals[2] = s.N - found; totals[3] = 0;
   }
   __syncthreads();
   const int limit = s.capacity ? s.capacity : s.N;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const int i = i0 + lane;
-    const int e = i < n ? ids[beg + i] : -1;
-    const bool ok = (unsigned)e < (unsigned)s.E;
-    const unsigned same = __match_any_sync(0xffffffffu, ok ? e : -1);
-    int r = 0;
-    if (ok) r = cnt[e] + __popc(same & ((1u << lane) - 1u));
-    __syncwarp();
-    if (ok && (same >> lane) == 1u) cnt[e] = r + 1;           // the last of its kind in this round
-    __syncwarp();
-    if (i < n) {
-      const int row = ok && r < limit ? start[e] + r : -1;
-      pos[beg + i] = row;
-      if (row >= 0) row_token[row] = (int)((beg + i) / s.k);
+  for (int i0 = 0; i0 < n; i0 += 128) {          // four rounds' ids are asked for at once
+    int id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + 32 * u + lane;
+      id[u] = i < n ? ids[beg + i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + 32 * u + lane, e = id[u];
+      if (i0 + 32 * u >= n) break;
+      const bool ok = (unsigned)e < (unsigned)s.E;
+      const unsigned same = __match_any_sync(0xffffffffu, ok ? e : -1);
+      int r = 0;
+      if (ok) r = cnt[e] + __popc(same & ((1u << lane) - 1u));
+      __syncwarp();
+      if (ok && (same >> lane) == 1u) cnt[e] = r + 1;         // the last of its kind in this round
+      __syncwarp();
+      if (i < n) {
+        const int row = ok && r < limit ? start[e] + r : -1;
+        pos[beg + i] = row;
+        if (row >= 0) row_token[row] = (int)((beg + i) / s.k);
+      }
     }
   }
   // rows without a token
-  for (int e = rank; e < s.E; e += ncta) {
+  for (int e = blockIdx.x; e < s.E; e += gridDim.x) {
     const int stop = e + 1 < s.E ? start[e + 1] : s.n_rows;
-    for (int r = start[e] + kept[e] + tid; r < stop; r += SORT_WARPS * 32) row_token[r] = -1;
+    for (int r = start[e] + kept[e] + tid; r < stop; r += threads) row_token[r] = -1;
   }
-  cluster.sync();                                // no CTA leaves while another may still read its counts
+  if (ncta > 1) cluster.sync();                  // no CTA leaves while another may still read its counts
 }
 
 // Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first PAD_SHARES * E blocks of a
@@ -173,61 +225,86 @@ sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, cons
   }
 }
 
-// Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.
+// Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.  A
+// thread has one 16-byte piece of a token and asks for UNSORT_AHEAD rows' pieces before it adds them.
+constexpr int UNSORT_AHEAD = 4;
 template <class T>
 __global__ void __launch_bounds__(256)
-unsort_kernel(const T* rows, const float* w, const int32_t* pos, T* __restrict__ Y, long long n, int ng, int k, int d) {
+unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv, int k) {
+  constexpr int P = PIECE<T>;
   grid_sync();
   const long long base = (long long)blockIdx.x * 256;
-  const long long t0 = base / ng;
-  const int i = (int)(base - t0 * ng) + (int)threadIdx.x;
+  const long long t0 = base / nv;
+  const int i = (int)(base - t0 * nv) + (int)threadIdx.x;
   if (base + (int)threadIdx.x >= n) return;
-  const unsigned dt = (unsigned)i / (unsigned)ng;
-  const int g = i - (int)dt * ng;
-  const long long t = t0 + dt;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < k; ++j) {
-    const int row = pos[t * k + j];
-    if (row < 0) continue;
-    const float f = w ? w[t * k + j] : 1.f;
-    const Vec8<T> o = Vec8<T>::load(rows + (size_t)row * d + (size_t)g * 8);
+  const unsigned dt = (unsigned)i / (unsigned)nv;
+  const int v = i - (int)dt * nv;
+  const long long first = (t0 + dt) * k;
+  float acc[P];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = fmaf(f, o.v[e], acc[e]);
+  for (int e = 0; e < P; ++e) acc[e] = 0.f;
+  for (int j0 = 0; j0 < k; j0 += UNSORT_AHEAD) {
+    int r[UNSORT_AHEAD];
+    uint4 q[UNSORT_AHEAD];
+    float f[UNSORT_AHEAD];
+#pragma unroll
+    for (int u = 0; u < UNSORT_AHEAD; ++u) r[u] = j0 + u < k ? pos[first + j0 + u] : -1;
+#pragma unroll
+    for (int u = 0; u < UNSORT_AHEAD; ++u) {
+      q[u] = r[u] >= 0 ? rows[(size_t)r[u] * nv + v] : make_uint4(0, 0, 0, 0);
+      f[u] = r[u] >= 0 && w ? w[first + j0 + u] : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < UNSORT_AHEAD; ++u) {
+      float x[P];
+      unpack<T>(q[u], x);
+#pragma unroll
+      for (int e = 0; e < P; ++e) acc[e] = fmaf(f[u], x[e], acc[e]);
+    }
   }
-  Vec8<T>::store(Y + (size_t)t * d + (size_t)g * 8, acc);
+  Y[base + (int)threadIdx.x] = pack<T>(acc);
 }
 
-// dO[pos[t][j]] = w[t][j] dY[t], dw[t][j] = <dY[t], O[pos[t][j]]>; a warp per pair.  The warps of a token are neighbours, so its
-// dY comes from HBM once.
+// dO[pos[t][j]] = w[t][j] dY[t], dw[t][j] = <dY[t], O[pos[t][j]]>; L lanes per pair (a warp, or the power of two that holds a
+// short row).  The pairs of a token are neighbours, so its dY comes from HBM once.
 template <class T>
 __global__ void __launch_bounds__(256)
-unsort_bwd_kernel(const T* dY, const T* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
-                  T* __restrict__ dO, float* __restrict__ dw, long long pairs, int k, int d, int align, int pad_blocks) {
+unsort_bwd_kernel(const uint4* dY, const uint4* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
+                  uint4* __restrict__ dO, float* __restrict__ dw, long long pairs, int k, int nv, int L, int align, int pad_blocks) {
+  constexpr int P = PIECE<T>, AHEAD = 4;
   grid_sync();
-  if ((int)blockIdx.x < pad_blocks)
-    return zero_pad_rows(reinterpret_cast<uint4*>(dO), d * (int)sizeof(T) / 16, counts, offsets, align);
-  const long long i = (long long)(blockIdx.x - pad_blocks) * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (i >= pairs) return;
-  const int row = pos[i];
-  if (row < 0) {
-    if (lane == 0) dw[i] = 0.f;
-    return;
-  }
-  const float f = w[i];
-  const T* gy = dY + (size_t)(i / k) * d;
-  const T* o = O + (size_t)row * d;
-  T* out = dO + (size_t)row * d;
+  if ((int)blockIdx.x < pad_blocks) return zero_pad_rows(dO, nv, counts, offsets, align);
+  const long long i = ((long long)(blockIdx.x - pad_blocks) * 256 + threadIdx.x) / L;
+  const int lane = threadIdx.x & (L - 1);
+  const int row = i < pairs ? pos[i] : -1;
   float dot = 0.f;
-  for (int v = lane; v < d / 8; v += 32) {
-    const Vec8<T> a = Vec8<T>::load(gy + v * 8), b = Vec8<T>::load(o + v * 8);
-    float r[8];
+  if (row >= 0) {
+    const float f = w[i];
+    const uint4* gy = dY + (size_t)(i / k) * nv;
+    const uint4* o = O + (size_t)row * nv;
+    uint4* out = dO + (size_t)row * nv;
+    for (int v0 = lane; v0 < nv; v0 += L * AHEAD) {
+      uint4 a[AHEAD], b[AHEAD];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { r[e] = f * a.v[e]; dot = fmaf(a.v[e], b.v[e], dot); }
-    Vec8<T>::store(out + v * 8, r);
+      for (int u = 0; u < AHEAD; ++u) {
+        const bool in = v0 + u * L < nv;
+        a[u] = in ? gy[v0 + u * L] : make_uint4(0, 0, 0, 0);
+        b[u] = in ? o[v0 + u * L] : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (v0 + u * L >= nv) continue;
+        float x[P], y[P];
+        unpack<T>(a[u], x);
+        unpack<T>(b[u], y);
+#pragma unroll
+        for (int e = 0; e < P; ++e) { dot = fmaf(x[e], y[e], dot); x[e] *= f; }
+        out[v0 + u * L] = pack<T>(x);
+      }
+    }
   }
-  dot = warp_sum(dot);
-  if (lane == 0) dw[i] = dot;
+  for (int s = L >> 1; s > 0; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
+  if (lane == 0 && i < pairs) dw[i] = dot;
 }
 
 // ---- launches ----------------------------------------------------------------------------------
@@ -250,10 +327,10 @@ static etr_status sort_valid(const etr_sort_config* c) {
 }
 
 static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* p, std::initializer_list<const void*> more) {
-  if (p == nullptr || p->counts == nullptr || p->offsets == nullptr || p->totals == nullptr) return ETR_ERR_ARG;
+  if (p == nullptr || p->counts == nullptr || p->offsets == nullptr || p->totals == nullptr || p->scratch == nullptr) return ETR_ERR_ARG;
   const bool rows = sort_rows_bound(c) > 0, some = c->T > 0;
   if ((rows && p->row_token == nullptr) || (some && p->pos == nullptr)) return ETR_ERR_ARG;
-  for (const void* q : {(const void*)p->counts, (const void*)p->offsets, (const void*)p->totals, (const void*)p->row_token, (const void*)p->pos})
+  for (const void* q : {(const void*)p->counts, (const void*)p->offsets, (const void*)p->totals, (const void*)p->row_token, (const void*)p->pos, (const void*)p->scratch})
     if (!aligned16(q)) return ETR_ERR_ALIGN;
   if (!some) return ETR_OK;                  // nothing is read or written through them
   for (const void* q : more) {
@@ -265,15 +342,32 @@ static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* 
 
 static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD_SHARES * c->E : 0; }
 
+// One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 8 of 16 warps; longer batches take up to 18 such
+// clusters, and a launch before that counts the clusters' pairs.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
-  const size_t smem = (size_t)(SORT_WARPS + 3) * c->E * 4;
-  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 3) * SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
-  const SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c)};
-  int ncta = 1;
-  while (ncta < SORT_MAX_CLUSTER && s.N > ncta * SORT_WARPS * 64) ncta *= 2;
+  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 3) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c), 0};
+  const int cta = SORT_WARPS * SORT_RUN, cluster = cta * SORT_CLUSTER;
+  int warps = SORT_WARPS, ncta = 1, nclusters = 1;
+  if (s.N <= cta) {
+    warps = std::max(std::max(ceil_div(s.N, 32), ceil_div(s.E, 64)), 4);
+    warps = std::min(warps, SORT_WARPS);
+  } else {
+    while (ncta < SORT_CLUSTER && s.N > ncta * cta) ncta *= 2;
+    nclusters = std::min((s.N + cluster - 1) / cluster, SORT_MAX_CLUSTERS);
+  }
+  const int all = warps * ncta * nclusters;
+  s.run = ((s.N + all - 1) / all + 31) & ~31;
+  if (nclusters > 1) {
+    ETR_TIME_BEGIN("sort_count_kernel");
+    launch_kernel(sort_count_kernel, nclusters * SORT_CLUSTER, SORT_WARPS * 32, (size_t)c->E * 4, st, SORT_CLUSTER, ids, s, p->scratch);
+    ETR_LAUNCH_CHECK();
+  }
+  const size_t smem = (size_t)(warps + 3) * c->E * 4;
   ETR_TIME_BEGIN("sort_plan_kernel");
-  launch_kernel(sort_plan_kernel, ncta, SORT_WARPS * 32, smem, st, ncta, ids, s, p->counts, p->offsets, p->totals, p->row_token, p->pos);
+  launch_kernel(sort_plan_kernel, nclusters * ncta, warps * 32, smem, st, ncta, ids, s, (const int32_t*)p->scratch, nclusters, p->counts,
+                p->offsets, p->totals, p->row_token, p->pos);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
 }
@@ -281,9 +375,11 @@ static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, cons
 template <class T>
 static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_plan* p, const void* a, const void* b, const float* w,
                             void* out, float* dw, cudaStream_t st) {
-  const int pad = sort_pad_blocks(c), nv = c->d * (int)sizeof(T) / 16, ng = c->d / 8;
-  const long long n = (long long)c->T * (which == 0 ? nv : ng), pairs = (long long)c->T * c->k;
-  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 255) / 256 : (pairs + 7) / 8;
+  const int pad = sort_pad_blocks(c), nv = c->d / PIECE<T>;
+  int L = 32;                                    // lanes per pair of unsort_bwd
+  while (L > 1 && nv <= L / 2) L /= 2;
+  const long long n = (long long)c->T * nv, pairs = (long long)c->T * c->k;
+  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 255) / 256 : (pairs * L + 255) / 256;
   if (blocks + pad >= (1ll << 31)) return ETR_ERR_SHAPE;
   switch (which) {
     case 0:
@@ -293,12 +389,12 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
       break;
     case 1:
       ETR_TIME_BEGIN("unsort_kernel");
-      launch_kernel(unsort_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const T*)a, w, p->pos, (T*)out, n, ng, c->k, c->d);
+      launch_kernel(unsort_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
       break;
     case 2:
       ETR_TIME_BEGIN("unsort_bwd_kernel");
-      launch_kernel(unsort_bwd_kernel<T>, (unsigned)(blocks + pad), 256, 0, st, 1, (const T*)a, (const T*)b, w, p->pos, p->counts,
-                    p->offsets, (T*)out, dw, pairs, c->k, c->d, c->align, pad);
+      launch_kernel(unsort_bwd_kernel<T>, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, (const uint4*)b, w, p->pos, p->counts,
+                    p->offsets, (uint4*)out, dw, pairs, c->k, nv, L, c->align, pad);
       break;
   }
   ETR_LAUNCH_CHECK();
@@ -334,6 +430,7 @@ etr_status etr_sort_plan_bind(const etr_sort_config* c, void* base, size_t bytes
   p.totals = take(4);
   p.row_token = take((size_t)sort_rows_bound(c));
   p.pos = take((size_t)c->T * c->k);
+  p.scratch = take((size_t)SORT_MAX_CLUSTERS * c->E);
   if (need) *need = off;
   if (out) {
     if (bytes < off) return ETR_ERR_WORKSPACE;

@@ -392,7 +392,7 @@ class SortConfig(C.Structure):
 
 
 class SortPlan(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("counts", "offsets", "totals", "row_token", "pos")]
+    _fields_ = [(n, C.c_void_p) for n in ("counts", "offsets", "totals", "row_token", "pos", "scratch")]
 
 
 SORT_MAX_K, SORT_MAX_E, NORM_MAX_D = 32, 1024, 16384

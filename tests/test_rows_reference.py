@@ -110,7 +110,7 @@ def test_sort_configurations(change, code):
         assert etr.sort_n_rows(cfg) == 0
         n = C.c_size_t(0)
         assert etr.lib().etr_sort_plan_bind(C.byref(cfg), None, C.c_size_t(0), None, C.byref(n)) == code
-        plan = etr.SortPlan(*[1 << 20] * 5)
+        plan = etr.SortPlan(*[1 << 20] * 6)
         assert etr.lib().etr_sort(C.addressof(cfg), 1 << 20, C.addressof(plan), None) == code
 
 
@@ -127,12 +127,12 @@ def test_sort_pointers_are_checked():
     a = C.addressof(cfg)
 
     def plan(**kw):
-        p = etr.SortPlan(*[ok] * 5)
+        p = etr.SortPlan(*[ok] * 6)
         for n, v in kw.items():
             setattr(p, n, v)
         return p
 
-    for name in ("counts", "offsets", "totals", "row_token", "pos"):
+    for name in ("counts", "offsets", "totals", "row_token", "pos", "scratch"):
         for value, code in ((None, etr.ERR_ARG), (ok + 4, etr.ERR_ALIGN)):
             p = plan(**{name: value})
             q = C.addressof(p)
