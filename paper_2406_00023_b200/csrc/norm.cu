@@ -25,316 +25,394 @@ struct RowShape { int tpr, rpb, stages; };
 
 // Sum over a row's threads, in every one of them.  Two arrays take turns from sum to sum, so that one barrier a sum is
 // enough: whoever writes an array again has passed the barrier of the sum between, and so has every reader.
-constexpr int NORM_MAX_WARPS = 16;                // 512 threads
+constexpr int NORM_MAX_WARPS = 16;                // of a row, 512 threads
+constexpr int NORM_WIDE_ROWS = 4;                 // rows of more than a warp in a block of about 256 threads
 struct RowSum {
-  float (*red)[NORM_MAX_WARPS];                   // [2][NORM_MAX_WARPS]
-  int tpr, turn;
+  float (*red)[NORM_WIDE_ROWS][NORM_MAX_WARPS];   // [2][rows][warps of a row], zeros behind a row's last warp
+  int tpr, row, turn;
+  __device__ __forceinline__ void init() {
+    if (tpr <= 32) return;
+    for (int i = threadIdx.x; i < 2 * NORM_WIDE_ROWS * NORM_MAX_WARPS; i += blockDim.x) (&red[0][0][0])[i] = 0.f;
+    __syncthreads();
+  }
   __device__ __forceinline__ float operator()(float v) {
     if (tpr <= 32) {
       for (int o = tpr >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       return v;
     }
     v = warp_sum(v);
-    const int warp = threadIdx.x >> 5, wpr = tpr >> 5, first = warp / wpr * wpr;
-    if ((threadIdx.x & 31) == 0) red[turn][warp] = v;
+    const int wpr = tpr >> 5;
+    float* mine = red[turn][row];
+    if ((threadIdx.x & 31) == 0) mine[(threadIdx.x >> 5) - row * wpr] = v;
     __syncthreads();
-    v = 0.f;
-#pragma unroll 4
-    for (int w = 0; w < wpr; ++w) v += red[turn][first + w];
+    const float4* q = reinterpret_cast<const float4*>(mine);
+    float4 s = q[0];
+    v = (s.x + s.y) + (s.z + s.w);
+    if (wpr > 4) {
+      s = q[1];
+      v += (s.x + s.y) + (s.z + s.w);
+      if (wpr > 8) {
+        const float4 a = q[2], c = q[3];
+        v += ((a.x + a.y) + (a.z + a.w)) + ((c.x + c.y) + (c.z + c.w));
+      }
+    }
     turn ^= 1;
     return v;
   }
 };
 
-template <int N>
-__device__ __forceinline__ void load_gain(const float* w, int col, float* out) {       // w == nullptr: ones
+// Two fp32 values a register pair and instruction (fma.rn.f32x2 and its kin): these kernels are bound by the instructions
+// they issue, not by the multipliers.
+__device__ __forceinline__ unsigned long long bits2(float2 v) { return *reinterpret_cast<unsigned long long*>(&v); }
+__device__ __forceinline__ float2 from2(unsigned long long v) { return *reinterpret_cast<float2*>(&v); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return from2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return from2(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+template <class T>
+__device__ __forceinline__ void unpack2(const uint4 q, float2* v) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  if (sizeof(T) == 4) {
+    v[0] = make_float2(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    v[1] = make_float2(__uint_as_float(w[2]), __uint_as_float(w[3]));
+  } else {
 #pragma unroll
-  for (int e = 0; e < N; e += 4) {
-    const float4 q = w ? *reinterpret_cast<const float4*>(w + col + e) : make_float4(1.f, 1.f, 1.f, 1.f);
-    out[e] = q.x; out[e + 1] = q.y; out[e + 2] = q.z; out[e + 3] = q.w;
+    for (int i = 0; i < 4; ++i) v[sizeof(T) == 4 ? 0 : i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+}
+template <class T>
+__device__ __forceinline__ uint4 pack2(const float2* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      w[i] = __float_as_uint(i & 1 ? v[i / 2].y : v[i / 2].x);
+    } else {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[sizeof(T) == 4 ? 0 : i].x, v[sizeof(T) == 4 ? 0 : i].y);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int H>                                  // H pairs from column col on; w == nullptr: ones
+__device__ __forceinline__ void load_gain(const float* w, int col, float2* out) {
+#pragma unroll
+  for (int e = 0; e < H; e += 2) {
+    const float4 q = w ? *reinterpret_cast<const float4*>(w + col + 2 * e) : make_float4(1.f, 1.f, 1.f, 1.f);
+    out[e] = make_float2(q.x, q.y);
+    out[e + 1] = make_float2(q.z, q.w);
   }
 }
 
 // The rows of up to NT tensors, tiles ahead of their use.  A thread copies (cp.async) exactly the pieces that it reads
-// itself, so that a wait for its own copies is all the synchronisation the ring needs.
-template <int NT, int NV>
+// itself, so that a wait for its own copies is all the synchronisation the ring needs.  Pieces behind a row's end and rows
+// behind the last arrive as zeros (a copy of no bytes).  RING false: rows so long that two tiles do not fit come straight
+// from global memory.
+template <int NT, int NV, bool RING>
 struct RowRing {
-  uint4* smem;
-  __device__ __forceinline__ uint4* slot(int stage, int tensor, int u) const { return smem + ((stage * NT + tensor) * NV + u) * blockDim.x + threadIdx.x; }
-  __device__ __forceinline__ void fetch(int stage, int tensor, int u, const uint4* src) const {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot(stage, tensor, u))), "l"(src) : "memory");
+  uint32_t smem;                                  // this thread's first slot
+  uint32_t pitch;                                 // between pieces, 16 bytes a thread
+  int stages, stage;
+  __device__ __forceinline__ uint32_t slot(int st, int tensor, int u) const { return smem + ((st * NT + tensor) * NV + u) * pitch; }
+  __device__ __forceinline__ void fetch(int st, int tensor, int u, const uint4* src, bool there) const {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot(st, tensor, u)), "l"(src), "r"(there ? 16 : 0) : "memory");
   }
   __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
   // all copies but those of the stages - 1 youngest tiles have arrived
-  __device__ __forceinline__ void wait(int stages) const {
+  __device__ __forceinline__ void wait() const {
     if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
     else asm volatile("cp.async.wait_group 1;" ::: "memory");
   }
+  __device__ __forceinline__ uint4 piece(int tensor, int u, const void* base, size_t at, bool there) const {
+    if (RING) {
+      uint4 q;
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(slot(stage, tensor, u)) : "memory");
+      return q;
+    }
+    return there ? ((const uint4*)base)[at] : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ int oldest() const { return stage == 0 ? stages - 1 : stage - 1; }       // free for a new tile
+  __device__ __forceinline__ void next() { stage = stage + 1 < stages ? stage + 1 : 0; }
 };
 
 // Forward: at most 80 registers a thread, so that 768 threads fit an SM; backward: 128 and 512.
 constexpr int NORM_FWD_REGS = 80, NORM_FWD_THREADS = 768, NORM_BWD_REGS = 128, NORM_BWD_THREADS = 512;
 
-// Forward.  JOIN false: prenorm of X.  Blocks walk tiles of RPB rows in strides, with the gains in registers.
+// Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.
 template <class T, int NV, bool RING, bool JOIN>
 __global__ void __maxnreg__(NV > 2 ? 128 : NORM_FWD_REGS)
 norm_fwd_kernel(const NormArgs p, const RowShape sh) {
-  constexpr int P = PIECE<T>, NT = JOIN ? 2 : 1;
+  constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 2 : 1, XX = 0, YY = NT - 1;
   extern __shared__ uint4 ring_smem[];
-  __shared__ float red[2][NORM_MAX_WARPS];
-  RowSum row_sum{red, sh.tpr, 0};
-  const RowRing<NT, NV> ring{ring_smem};
-  const int TPR = sh.tpr, RPB = sh.rpb, S = sh.stages;
-  const int row = threadIdx.x / TPR, tg = threadIdx.x - row * TPR, np = p.d / P;
+  __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
+  const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
+  RowSum row_sum{red, tpr, row, 0};
+  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, sh.stages, 0};
   const float inv_d = 1.f / (float)p.d;
-  const long long step = (long long)gridDim.x * RPB;
-  auto fetch = [&](int stage, long long t) {
-    if (t < p.T) {
-      const size_t off = (size_t)t * np;
+  const int step = gridDim.x * sh.rpb;
+  const size_t stride = (size_t)step * np;
+  bool in[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) in[u] = tg + u * tpr < np;
+  auto fetch = [&](int st, long long tile, size_t at) {      // tile: its first row; at: this thread's first piece
+    if (tile < p.T) {
+      const bool live = tile + row < p.T;
+      const size_t a = live ? at : 0;
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int g = tg + u * TPR;
-        if (g >= np) continue;
-        if (JOIN) ring.fetch(stage, NT - 1, u, (const uint4*)p.Y + off + g);
-        ring.fetch(stage, 0, u, (const uint4*)p.X + off + g);
+        const size_t i = in[u] && live ? a + u * tpr : 0;
+        if (JOIN) ring.fetch(st, YY, u, (const uint4*)p.Y + i, live && in[u]);
+        ring.fetch(st, XX, u, (const uint4*)p.X + i, live && in[u]);
       }
     }
     ring.commit();
   };
+  row_sum.init();
   grid_sync();
-  long long t = (long long)blockIdx.x * RPB + row;
+  long long tile = (long long)blockIdx.x * sh.rpb;
+  size_t at = (size_t)(tile + row) * np + tg, ahead = at;
   if (RING)
-    for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
-  float wp[JOIN ? NV : 1][P], wn[NV][P];
+    for (int i = 0; i < sh.stages - 1; ++i, ahead += stride) fetch(i, tile + (long long)i * step, ahead);
+  float2 wp[JOIN ? NV : 1][H], wn[NV][H];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    const int g = min(tg + u * TPR, np - 1);
-    if (JOIN) load_gain<P>(p.w_post, g * P, wp[u]);
-    load_gain<P>(p.N ? p.w_next : nullptr, g * P, wn[u]);
+    const int g = min(tg + u * tpr, np - 1);
+    if (JOIN) load_gain<H>(in[u] ? p.w_post : nullptr, g * P, wp[u]);
+    load_gain<H>(in[u] && p.N ? p.w_next : nullptr, g * P, wn[u]);
   }
-  float gate = p.gate && t < p.T ? p.gate[t] : 1.f;
-  int stage = 0;
-  for (long long tb = (long long)blockIdx.x * RPB; tb < p.T; tb += step, t += step) {
+  const bool gated = JOIN && p.gate != nullptr;
+  float gate = gated && tile + row < p.T ? p.gate[tile + row] : 1.f;
+  for (; tile < p.T; tile += step, at += stride, ring.next()) {
+    const long long t = tile + row;
     const bool live = t < p.T;
-    const size_t off = (size_t)(live ? t : 0) * np;
     if (RING) {
-      fetch(stage == 0 ? S - 1 : stage - 1, t + (S - 1) * step);
-      ring.wait(S);
+      fetch(ring.oldest(), tile + (long long)(sh.stages - 1) * step, ahead);
+      ahead += stride;
+      ring.wait();
     }
-    auto piece = [&](int tensor, const void* base, int u) {
-      const int g = tg + u * TPR;
-      if (!live || g >= np) return make_uint4(0, 0, 0, 0);
-      return RING ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
-    };
-    float x[NV][P];
-#pragma unroll
-    for (int u = 0; u < NV; ++u) unpack<T>(piece(0, p.X, u), x[u]);
+    float2 x[NV][H];
     if (JOIN) {
-      float y[NV][P], f = p.b * gate;
+      float2 y[NV][H];
+      float f = p.b * gate;
+      if (gated && t + step < p.T) gate = p.gate[t + step];
 #pragma unroll
-      for (int u = 0; u < NV; ++u) unpack<T>(piece(NT - 1, p.Y, u), y[u]);
-      if (p.gate && t + step < p.T) gate = p.gate[t + step];
+      for (int u = 0; u < NV; ++u) unpack2<T>(ring.piece(YY, u, p.Y, at + u * tpr, live && in[u]), y[u]);
       if (p.post) {
-        float s = 0.f;
+        float2 s = both(0.f);
 #pragma unroll
         for (int u = 0; u < NV; ++u)
 #pragma unroll
-          for (int e = 0; e < P; ++e) s = fmaf(y[u][e], y[u][e], s);
-        const float r = rsqrtf(row_sum(s) * inv_d + p.eps);
+          for (int e = 0; e < H; ++e) s = fma2(y[u][e], y[u][e], s);
+        const float r = rsqrtf(row_sum(s.x + s.y) * inv_d + p.eps);
         if (p.rstd_y_out && live && tg == 0) p.rstd_y_out[t] = r;
         f *= r;
       }
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
+        unpack2<T>(ring.piece(XX, u, p.X, at + u * tpr, live && in[u]), x[u]);
 #pragma unroll
-        for (int e = 0; e < P; ++e) x[u][e] = fmaf(f * y[u][e], wp[u][e], p.a * x[u][e]);
-        const int g = tg + u * TPR;
-        if (live && g < np) ((uint4*)p.Xo)[off + g] = pack<T>(x[u]);
+        for (int e = 0; e < H; ++e) x[u][e] = fma2(mul2(y[u][e], both(f)), wp[u][e], mul2(x[u][e], both(p.a)));
+        if (live && in[u]) ((uint4*)p.Xo)[at + u * tpr] = pack2<T>(x[u]);
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) unpack2<T>(ring.piece(XX, u, p.X, at + u * tpr, live && in[u]), x[u]);
     }
     if (p.N) {
-      float s = 0.f;
+      float2 s = both(0.f);
 #pragma unroll
       for (int u = 0; u < NV; ++u)
 #pragma unroll
-        for (int e = 0; e < P; ++e) s = fmaf(x[u][e], x[u][e], s);
-      const float r = rsqrtf(row_sum(s) * inv_d + p.eps);
+        for (int e = 0; e < H; ++e) s = fma2(x[u][e], x[u][e], s);
+      const float r = rsqrtf(row_sum(s.x + s.y) * inv_d + p.eps);
       if (p.rstd_o_out && live && tg == 0) p.rstd_o_out[t] = r;
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int g = tg + u * TPR;
-        if (!live || g >= np) continue;
 #pragma unroll
-        for (int e = 0; e < P; ++e) x[u][e] *= r * wn[u][e];
-        ((uint4*)p.N)[off + g] = pack<T>(x[u]);
+        for (int e = 0; e < H; ++e) x[u][e] = mul2(mul2(x[u][e], both(r)), wn[u][e]);
+        if (live && in[u]) ((uint4*)p.N)[at + u * tpr] = pack2<T>(x[u]);
       }
     }
-    stage = stage + 1 < S ? stage + 1 : 0;
   }
 }
 
-// Backward.  Blocks walk tiles of RPB rows in strides, a thread always on the same columns, so the gains' gradients add up in
+// Backward.  Blocks walk tiles of rpb rows in strides, a thread always on the same columns, so the gains' gradients add up in
 // registers; a block leaves one row of partial sums per gain, which norm_dw_kernel adds in order.
 // JOIN false: prenorm (Xo_in is its input X, dXo the gradient that comes along the residual, may be NULL; no y).
+// The factors that are the same for a whole row (r_o, r_y, gate, a, b) are taken out of the sums over it:
+//   s1 = <w_next dN, x>,  G = dXo + r_o w_next dN - (r_o^2 (r_o s1 / d)) x,   s2 = <w_post G, y>,  dgate = b r_y s2,
+//   dY = (b gate r_y) w_post G - (b gate r_y (r_y (r_y s2 / d))) y
 template <class T, int NV, bool RING, bool JOIN>
 __global__ void __maxnreg__(NORM_BWD_REGS)
 norm_bwd_kernel(const NormArgs p, const RowShape sh) {
-  constexpr int P = PIECE<T>, NT = JOIN ? 4 : 3;
-  extern __shared__ uint4 ring_smem[];
-  __shared__ float red[2][NORM_MAX_WARPS];
-  RowSum row_sum{red, sh.tpr, 0};
-  const RowRing<NT, NV> ring{ring_smem};
-  const int TPR = sh.tpr, RPB = sh.rpb, S = sh.stages;
-  const int row = threadIdx.x / TPR, tg = threadIdx.x - row * TPR, np = p.d / P;
-  const float inv_d = 1.f / (float)p.d;
-  const long long step = (long long)gridDim.x * RPB;
+  constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 4 : 3;
   enum { DN, XO, DXO, YY };
-  auto fetch = [&](int stage, long long t) {
-    if (t < p.T) {
-      const size_t off = (size_t)t * np;
+  extern __shared__ uint4 ring_smem[];
+  __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
+  const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
+  RowSum row_sum{red, tpr, row, 0};
+  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, sh.stages, 0};
+  const float inv_d = 1.f / (float)p.d;
+  const int step = gridDim.x * sh.rpb;
+  const size_t stride = (size_t)step * np;
+  bool in[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) in[u] = tg + u * tpr < np;
+  auto fetch = [&](int st, long long tile, size_t at) {
+    if (tile < p.T) {
+      const bool live = tile + row < p.T;
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int g = tg + u * TPR;
-        if (g >= np) continue;
+        const bool there = live && in[u];
+        const size_t i = there ? at + u * tpr : 0;
         if (p.dN) {
-          ring.fetch(stage, DN, u, (const uint4*)p.dN + off + g);
-          ring.fetch(stage, XO, u, (const uint4*)p.Xo_in + off + g);
+          ring.fetch(st, DN, u, (const uint4*)p.dN + i, there);
+          ring.fetch(st, XO, u, (const uint4*)p.Xo_in + i, there);
         }
-        if (p.dXo) ring.fetch(stage, DXO, u, (const uint4*)p.dXo + off + g);
-        if (JOIN) ring.fetch(stage, YY, u, (const uint4*)p.Y + off + g);
+        if (p.dXo) ring.fetch(st, DXO, u, (const uint4*)p.dXo + i, there);
+        if (JOIN) ring.fetch(st, YY, u, (const uint4*)p.Y + i, there);
       }
     }
     ring.commit();
   };
+  row_sum.init();
   grid_sync();
-  long long t = (long long)blockIdx.x * RPB + row;
+  long long tile = (long long)blockIdx.x * sh.rpb;
+  size_t at = (size_t)(tile + row) * np + tg, ahead = at;
   if (RING)
-    for (int i = 0; i < S - 1; ++i) fetch(i, t + i * step);
-  float wp[JOIN ? NV : 1][P], wn[NV][P], acc_p[JOIN ? NV : 1][P], acc_n[NV][P];
+    for (int i = 0; i < sh.stages - 1; ++i, ahead += stride) fetch(i, tile + (long long)i * step, ahead);
+  float2 wp[JOIN ? NV : 1][H], wn[NV][H], acc_p[JOIN ? NV : 1][H], acc_n[NV][H];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    const int g = min(tg + u * TPR, np - 1);
-    load_gain<P>(p.dN ? p.w_next : nullptr, g * P, wn[u]);
-    if (JOIN) load_gain<P>(p.w_post, g * P, wp[u]);
+    const int g = min(tg + u * tpr, np - 1);
+    load_gain<H>(in[u] && p.dN ? p.w_next : nullptr, g * P, wn[u]);
+    if (JOIN) load_gain<H>(in[u] ? p.w_post : nullptr, g * P, wp[u]);
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-      acc_n[u][e] = 0.f;
-      if (JOIN) acc_p[u][e] = 0.f;
+    for (int e = 0; e < H; ++e) {
+      acc_n[u][e] = both(0.f);
+      if (JOIN) acc_p[u][e] = both(0.f);
     }
   }
   // a row's scalars are asked for one tile ahead
   float r_o = 0.f, r_y = 1.f, gate = 1.f;
-  auto scalars = [&](long long at) {
-    if (at >= p.T) return;
-    if (p.dN) r_o = p.rstd_o[at];
-    if (JOIN && p.post) r_y = p.rstd_y[at];
-    if (JOIN && p.gate) gate = p.gate[at];
+  auto scalars = [&](long long t) {
+    if (t >= p.T) return;
+    if (p.dN) r_o = p.rstd_o[t];
+    if (JOIN && p.post) r_y = p.rstd_y[t];
+    if (JOIN && p.gate) gate = p.gate[t];
   };
-  scalars(t);
-  int stage = 0;
-  for (long long tb = (long long)blockIdx.x * RPB; tb < p.T; tb += step, t += step) {
+  scalars(tile + row);
+  for (; tile < p.T; tile += step, at += stride, ring.next()) {
+    const long long t = tile + row;
     const bool live = t < p.T;
-    const size_t off = (size_t)(live ? t : 0) * np;
     const float ro = r_o, ry = r_y, ga = gate;
     scalars(t + step);
     if (RING) {
-      fetch(stage == 0 ? S - 1 : stage - 1, t + (S - 1) * step);
-      ring.wait(S);
+      fetch(ring.oldest(), tile + (long long)(sh.stages - 1) * step, ahead);
+      ahead += stride;
+      ring.wait();
     }
-    auto piece = [&](int tensor, const void* base, int u) {
-      const int g = tg + u * TPR;
-      if (base == nullptr || !live || g >= np) return make_uint4(0, 0, 0, 0);
-      return RING ? *ring.slot(stage, tensor, u) : ((const uint4*)base)[off + g];
-    };
-    float G[NV][P];
-#pragma unroll
-    for (int u = 0; u < NV; ++u) unpack<T>(piece(DXO, p.dXo, u), G[u]);
+    float2 G[NV][H];
     if (p.dN) {
-      float s = 0.f;
+      float2 s = both(0.f);
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        float dn[P], x[P];
-        unpack<T>(piece(DN, p.dN, u), dn);
-        unpack<T>(piece(XO, p.Xo_in, u), x);
+        float2 x[H];
+        unpack2<T>(ring.piece(DN, u, p.dN, at + u * tpr, live && in[u]), G[u]);
+        unpack2<T>(ring.piece(XO, u, p.Xo_in, at + u * tpr, live && in[u]), x);
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float q = dn[e] * (x[e] * ro);
-          acc_n[u][e] += q;
-          s = fmaf(q, wn[u][e], s);
+        for (int e = 0; e < H; ++e) {
+          acc_n[u][e] = fma2(mul2(G[u][e], x[e]), both(ro), acc_n[u][e]);
+          G[u][e] = mul2(G[u][e], wn[u][e]);
+          s = fma2(G[u][e], x[e], s);
         }
       }
-      s = row_sum(s) * inv_d;
+      const float c = -ro * (ro * (ro * row_sum(s.x + s.y) * inv_d));
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        float dn[P], x[P];
-        unpack<T>(piece(DN, p.dN, u), dn);
-        unpack<T>(piece(XO, p.Xo_in, u), x);
+        float2 x[H], o[H];
+        unpack2<T>(ring.piece(XO, u, p.Xo_in, at + u * tpr, live && in[u]), x);
+        if (p.dXo) {
+          unpack2<T>(ring.piece(DXO, u, p.dXo, at + u * tpr, live && in[u]), o);
 #pragma unroll
-        for (int e = 0; e < P; ++e) G[u][e] = fmaf(ro, fmaf(-(x[e] * ro), s, dn[e] * wn[u][e]), G[u][e]);
+          for (int e = 0; e < H; ++e) x[e] = fma2(x[e], both(c), o[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < H; ++e) x[e] = mul2(x[e], both(c));
+        }
+#pragma unroll
+        for (int e = 0; e < H; ++e) G[u][e] = fma2(G[u][e], both(ro), x[e]);
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) unpack2<T>(ring.piece(DXO, u, p.dXo, at + u * tpr, live && in[u]), G[u]);
     }
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int g = tg + u * TPR;
-      if (!live || g >= np) continue;
-      float out[P];
+      float2 out[H];
 #pragma unroll
-      for (int e = 0; e < P; ++e) out[e] = JOIN ? p.a * G[u][e] : G[u][e];
-      ((uint4*)p.dX)[off + g] = pack<T>(out);
+      for (int e = 0; e < H; ++e) out[e] = JOIN ? mul2(G[u][e], both(p.a)) : G[u][e];
+      if (live && in[u]) ((uint4*)p.dX)[at + u * tpr] = pack2<T>(out);
     }
     if (JOIN) {
-      float s = 0.f;
+      const float f = p.b * ga * ry;
+      float2 s = both(0.f);
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        float y[P];
-        unpack<T>(piece(YY, p.Y, u), y);
+        float2 y[H];
+        unpack2<T>(ring.piece(YY, u, p.Y, at + u * tpr, live && in[u]), y);
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float q = p.b * G[u][e] * (y[e] * ry);
-          acc_p[u][e] = fmaf(ga, q, acc_p[u][e]);
-          s = fmaf(q, wp[u][e], s);
+        for (int e = 0; e < H; ++e) {
+          acc_p[u][e] = fma2(mul2(G[u][e], y[e]), both(f), acc_p[u][e]);
+          G[u][e] = mul2(G[u][e], wp[u][e]);
+          s = fma2(G[u][e], y[e], s);
         }
       }
-      s = row_sum(s);
-      if (p.dgate && live && tg == 0) p.dgate[t] = s;
-      const float c = p.post ? s * inv_d : 0.f, f = ga * ry;
+      const float s2 = ry * row_sum(s.x + s.y);
+      if (p.dgate && live && tg == 0) p.dgate[t] = p.b * s2;
+      const float c = p.post ? -f * (ry * (s2 * inv_d)) : 0.f;
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int g = tg + u * TPR;
-        if (!live || g >= np) continue;
-        float y[P];
-        unpack<T>(piece(YY, p.Y, u), y);
+        float2 y[H];
+        unpack2<T>(ring.piece(YY, u, p.Y, at + u * tpr, live && in[u]), y);
 #pragma unroll
-        for (int e = 0; e < P; ++e) y[e] = f * fmaf(-(y[e] * ry), c, p.b * G[u][e] * wp[u][e]);
-        ((uint4*)p.dY)[off + g] = pack<T>(y);
+        for (int e = 0; e < H; ++e) y[e] = fma2(G[u][e], both(f), mul2(y[e], both(c)));
+        if (live && in[u]) ((uint4*)p.dY)[at + u * tpr] = pack2<T>(y);
       }
     }
-    stage = stage + 1 < S ? stage + 1 : 0;
   }
-  // One row of partial sums per block and gain; where a block has several row groups they are added first, through the
-  // ring's memory (every copy into it has arrived: the last groups waited for are empty).
+  // One row of partial sums per block and gain; where a block has several rows they are added first, through the ring's
+  // memory (every copy into it has arrived: the last groups waited for are empty).
   float* fold = reinterpret_cast<float*>(ring_smem);
 #pragma unroll
   for (int which = 0; which < (JOIN ? 2 : 1); ++which) {
     float* part = which ? p.part_post : p.part_next;
     if (part == nullptr) continue;
-    if (RPB > 1) __syncthreads();
+    if (sh.rpb > 1) __syncthreads();
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int g = tg + u * TPR;
-      if (g >= np) continue;
-      float* dst = RPB > 1 ? fold + (size_t)row * p.d + g * P : part + (size_t)blockIdx.x * p.d + g * P;
+      if (!in[u]) continue;
+      const int g = (tg + u * tpr) * P;
+      float* dst = sh.rpb > 1 ? fold + (size_t)row * p.d + g : part + (size_t)blockIdx.x * p.d + g;
 #pragma unroll
-      for (int e = 0; e < P; e += 4) {
-        const float* v = which ? acc_p[JOIN ? u : 0] : acc_n[u];
-        *reinterpret_cast<float4*>(dst + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+      for (int e = 0; e < H; e += 2) {
+        const float2 *v = which ? acc_p[JOIN ? u : 0] : acc_n[u];
+        *reinterpret_cast<float4*>(dst + 2 * e) = make_float4(v[e].x, v[e].y, v[e + 1].x, v[e + 1].y);
       }
     }
-    if (RPB > 1) {
+    if (sh.rpb > 1) {
       __syncthreads();
       for (int c = threadIdx.x; c < p.d; c += blockDim.x) {
         float s = 0.f;
-        for (int q = 0; q < RPB; ++q) s += fold[(size_t)q * p.d + c];
+        for (int q = 0; q < sh.rpb; ++q) s += fold[(size_t)q * p.d + c];
         part[(size_t)blockIdx.x * p.d + c] = s;
       }
     }
@@ -382,15 +460,14 @@ static etr_status norm_ptrs(std::initializer_list<const void*> need, std::initia
   return ETR_OK;
 }
 
-// Rows on threads.  2 pieces a thread where that is whole warps (one piece for rows within a warp), 4 or 8 where 512 threads
-// would not hold the row; about 256 threads a block.
+// Rows on threads.  2 pieces a thread, 4 or 8 where 512 threads would not hold the row; about 256 threads a block.
 static int norm_pieces(int d, int dtype) { return d * (int)elem_bytes(dtype) / 16; }
-static int norm_nv(int pieces) { return pieces <= 32 ? 1 : pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8; }
+static int norm_nv(int pieces) { return pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8; }
 static RowShape norm_shape(int pieces) {
   const int nv = norm_nv(pieces);
   RowShape s = {4, 1, 0};
-  if (nv == 1)
-    while (s.tpr < pieces) s.tpr *= 2;
+  if (pieces <= 64)
+    while (2 * s.tpr < pieces) s.tpr *= 2;
   else
     s.tpr = ceil_div(pieces, 32 * nv) * 32;
   s.rpb = s.tpr < 256 ? 256 / s.tpr : 1;
@@ -402,7 +479,6 @@ static etr_status norm_by_shape(const NormArgs& p, cudaStream_t st) {
   const int pieces = p.d / PIECE<T>;
   const RowShape s = norm_shape(pieces);
   switch (norm_nv(pieces)) {
-    case 1: return K<T, 1>::run(p, s, st);
     case 2: return K<T, 2>::run(p, s, st);
     case 4: return K<T, 4>::run(p, s, st);
   }
