@@ -13,6 +13,7 @@ namespace etr {
 constexpr int SORT_WARPS = 16;                   // at most
 constexpr int SORT_CLUSTER = 8;
 constexpr int SORT_MAX_CLUSTERS = 18;            // 144 of the 148 SMs
+constexpr int SORT_ONE_CLUSTER = 32768;          // pairs that one cluster takes without a counting launch before it
 constexpr int SORT_RUN = 64;                     // pairs per warp that are worth another CTA
 
 struct SortShape {
@@ -226,10 +227,10 @@ sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, cons
 }
 
 // Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.  A
-// thread has one 16-byte piece of a token and asks for UNSORT_AHEAD rows' pieces before it adds them.
-constexpr int UNSORT_AHEAD = 4;
-template <class T>
-__global__ void __launch_bounds__(256)
+// thread has one 16-byte piece of a token and asks for AHEAD rows' pieces before it adds them: 2 at full occupancy for k <= 2, else 4
+// at three quarters of it (65536 x 4096 bf16, k = 2: 302 and 322 us; 6113 x 2048, k = 8: 41 and 36.5).
+template <class T, int AHEAD>
+__global__ void __launch_bounds__(256, AHEAD > 2 ? 6 : 8)
 unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv, int k) {
   constexpr int P = PIECE<T>;
   grid_sync();
@@ -239,27 +240,26 @@ unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __re
   if (base + (int)threadIdx.x >= n) return;
   const unsigned dt = (unsigned)i / (unsigned)nv;
   const int v = i - (int)dt * nv;
-  const long long first = (t0 + dt) * k;
+  const int32_t* p = pos + (t0 + dt) * k;
+  const float* f = w ? w + (t0 + dt) * k : nullptr;
+  rows += v;
   float acc[P];
 #pragma unroll
   for (int e = 0; e < P; ++e) acc[e] = 0.f;
-  for (int j0 = 0; j0 < k; j0 += UNSORT_AHEAD) {
-    int r[UNSORT_AHEAD];
-    uint4 q[UNSORT_AHEAD];
-    float f[UNSORT_AHEAD];
+  for (int j0 = 0; j0 < k; j0 += AHEAD) {
+    int r[AHEAD];
+    uint4 q[AHEAD];
 #pragma unroll
-    for (int u = 0; u < UNSORT_AHEAD; ++u) r[u] = j0 + u < k ? pos[first + j0 + u] : -1;
+    for (int u = 0; u < AHEAD; ++u) r[u] = j0 + u < k ? p[j0 + u] : -1;
 #pragma unroll
-    for (int u = 0; u < UNSORT_AHEAD; ++u) {
-      q[u] = r[u] >= 0 ? rows[(size_t)r[u] * nv + v] : make_uint4(0, 0, 0, 0);
-      f[u] = r[u] >= 0 && w ? w[first + j0 + u] : 1.f;
-    }
+    for (int u = 0; u < AHEAD; ++u) q[u] = r[u] >= 0 ? rows[(size_t)r[u] * nv] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int u = 0; u < UNSORT_AHEAD; ++u) {
+    for (int u = 0; u < AHEAD; ++u) {
+      const float g = r[u] >= 0 && f ? f[j0 + u] : 1.f;
       float x[P];
       unpack<T>(q[u], x);
 #pragma unroll
-      for (int e = 0; e < P; ++e) acc[e] = fmaf(f[u], x[e], acc[e]);
+      for (int e = 0; e < P; ++e) acc[e] = fmaf(g, x[e], acc[e]);
     }
   }
   Y[base + (int)threadIdx.x] = pack<T>(acc);
@@ -343,7 +343,8 @@ static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* 
 static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD_SHARES * c->E : 0; }
 
 // One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 8 of 16 warps; longer batches take up to 18 such
-// clusters, and a launch before that counts the clusters' pairs.
+// clusters, and a launch before that counts the clusters' pairs.  Measured with the rows of d = 64 behind it: 32768
+// pairs 13.9 us in one cluster, 16.6 with the count; 65536 17.2 and 16.3; 131072 26.5 and 19.8; 524288 94 and 41.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
   if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 3) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
@@ -355,7 +356,7 @@ static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, cons
     warps = std::min(warps, SORT_WARPS);
   } else {
     while (ncta < SORT_CLUSTER && s.N > ncta * cta) ncta *= 2;
-    nclusters = std::min((s.N + cluster - 1) / cluster, SORT_MAX_CLUSTERS);
+    if (s.N > SORT_ONE_CLUSTER) nclusters = std::min((s.N + cluster - 1) / cluster, SORT_MAX_CLUSTERS);
   }
   const int all = warps * ncta * nclusters;
   s.run = ((s.N + all - 1) / all + 31) & ~31;
@@ -379,7 +380,7 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   int L = 32;                                    // lanes per pair of unsort_bwd
   while (L > 1 && nv <= L / 2) L /= 2;
   const long long n = (long long)c->T * nv, pairs = (long long)c->T * c->k;
-  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 255) / 256 : (pairs * L + 255) / 256;
+  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 256 - 1) / 256 : (pairs * L + 255) / 256;
   if (blocks + pad >= (1ll << 31)) return ETR_ERR_SHAPE;
   switch (which) {
     case 0:
@@ -389,7 +390,7 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
       break;
     case 1:
       ETR_TIME_BEGIN("unsort_kernel");
-      launch_kernel(unsort_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
+      launch_kernel(c->k > 2 ? unsort_kernel<T, 4> : unsort_kernel<T, 2>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
       break;
     case 2:
       ETR_TIME_BEGIN("unsort_bwd_kernel");
