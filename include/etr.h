@@ -471,6 +471,19 @@ etr_status etr_unsort_rows(const etr_sort_config* cfg, const void* O, const floa
 etr_status etr_unsort_rows_bwd(const etr_sort_config* cfg, const void* dY, const void* O, const float* weights,
                                const etr_sort_plan* plan, void* dO, float* dweights, void* stream);
 
+/* The layer's experts under a choice and weights that the caller's router made: etr_sort in the layer's layout (align 128,
+ * capacity cfg->capacity), etr_sort_rows into buf->Xp, etr_expert_ffn, etr_unsort_rows of buf->O, in that order, and
+ * etr_unsort_rows_bwd, etr_expert_ffn_bwd, etr_sort_rows_bwd on the buffers and the plan that the forward call filled.
+ * cfg is the layer's (k <= ETR_SORT_MAX_K); its D, mode, step, adaptive, gate, threshold and fuse members are not used.
+ * buf->stats is cleared, and afterwards holds only the error word.  plan: etr_sort_plan_bind of
+ * {T, k, E, d, dtype, 128, capacity}.  With capacity = T nothing is dropped whatever the choice. */
+etr_status etr_routed_forward(const etr_config* cfg, const void* X, const int32_t* topk_idx, const float* weights,
+                              const void* W1g, const void* W1u, const void* W2, const etr_buffers* buf,
+                              const etr_sort_plan* plan, void* Y, void* stream);
+etr_status etr_routed_backward(const etr_config* cfg, const float* weights, const void* W1g, const void* W1u, const void* W2,
+                               const void* dY, const etr_buffers* buf, const etr_sort_plan* plan, void* dX, float* dweights,
+                               void* dW1g, void* dW1u, void* dW2, void* stream);
+
 /* ---- the norm before a block and the join behind it ------------------------------------------------- */
 
 /* Rows of d values (d % 8 == 0, d <= ETR_NORM_MAX_D) of `dtype`; gains, gates, 1/rms and their gradients fp32; pointers 16-byte
@@ -510,6 +523,27 @@ etr_status etr_join(const etr_norm_config* cfg, const void* X, const void* Y, co
 etr_status etr_join_bwd(const etr_norm_config* cfg, const void* dXo, const void* dN, const void* Y, const void* Xo,
                         const float* w_post, const float* gate, const float* w_next, const float* rstd_y, const float* rstd_o,
                         void* dX, void* dY, float* dw_post, float* dgate, float* dw_next, void* ws, void* stream);
+
+/* A block: the norm, the layer and the join around it as one call each way.
+ *   N = prenorm(X, w_pre);  Y = layer(N);  Xo = a X + b gate w_post norm(Y)
+ * ncfg has cfg's T, d and dtype (ETR_ERR_SHAPE otherwise).  X is read again by the backward call, which may write dX over
+ * dXo; Xo may be X only where no backward call follows.  dgate, dw_pre and dw_post may be NULL. */
+typedef struct etr_block_buffers {
+  void* N; void* Y;           /* [T,d] the layer's input and output */
+  void* dN; void* dY;         /* [T,d] their gradients */
+  float* rstd_x; float* rstd_y;   /* [T] */
+  void* ws;                   /* etr_norm_workspace_bytes */
+} etr_block_buffers;
+/* Size of a block of memory for them (need, may be NULL) and its carving (out, may be NULL; base 256-byte aligned). */
+etr_status etr_block_bind(const etr_norm_config* ncfg, void* base, size_t bytes, etr_block_buffers* out, size_t* need);
+etr_status etr_block_forward(const etr_config* cfg, const etr_norm_config* ncfg, const void* X, const float* w_pre,
+                             const float* w_post, const float* gate, const float* R, const void* W1g, const void* W1u,
+                             const void* W2, const etr_buffers* buf, const etr_block_buffers* bb, void* Xo, void* stream);
+etr_status etr_block_backward(const etr_config* cfg, const etr_norm_config* ncfg, const void* X, const float* w_pre,
+                              const float* w_post, const float* gate, const float* R, const void* W1g, const void* W1u,
+                              const void* W2, const void* dXo, const etr_buffers* buf, const etr_block_buffers* bb, void* dX,
+                              float* dw_pre, float* dw_post, float* dgate, float* dR, void* dW1g, void* dW1u, void* dW2,
+                              void* stream);
 
 /* Number of kernels launched by this library in the calling process so far. */
 int64_t etr_launch_count(void);

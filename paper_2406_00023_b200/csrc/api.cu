@@ -493,6 +493,108 @@ etr_status etr_layer_backward(const etr_config* c, const void* X, const float* R
                            b->dXp, dX, dR, b->ws, b->stats, (cudaStream_t)stream);
 }
 
+// ---- the experts under the caller's own choice ---------------------------------------------------
+static etr_sort_config routed_sort_config(const etr_config* c) {
+  return etr_sort_config{c->T, c->k, c->E, c->d, c->dtype, 128, c->capacity, 0};
+}
+// The layer's route with the plan's rows: what the expert GEMMs read of it.
+static etr_status routed_route(const etr_buffers* b, const etr_sort_plan* p, etr_route* out) {
+  if (b == nullptr || p == nullptr) return ETR_ERR_ARG;
+  *out = b->route;
+  out->counts = p->counts;
+  out->slot_token = p->row_token;
+  return check_route(out);
+}
+
+etr_status etr_routed_forward(const etr_config* c, const void* X, const int32_t* topk_idx, const float* weights, const void* W1g,
+                              const void* W1u, const void* W2, const etr_buffers* b, const etr_sort_plan* plan, void* Y, void* stream) {
+  ETR_TRY(etr_validate(c));
+  etr_route route;
+  ETR_TRY(routed_route(b, plan, &route));
+  ETR_TRY(check_ptrs({X, topk_idx, weights, W1g, W1u, W2, b->stats, b->Xp, b->G, b->U, b->H, b->O, b->ws, Y}));
+  ETR_TRY(check_workspace(c, b, false, false));
+  const etr_sort_config s = routed_sort_config(c);
+  ETR_TRY(etr_sort_validate(&s));
+  if (cudaMemsetAsync(b->stats, 0, sizeof(etr_stats), (cudaStream_t)stream) != cudaSuccess) return ETR_ERR_CUDA;
+  ETR_TRY(etr_sort(&s, topk_idx, plan, stream));
+  ETR_TRY(etr_sort_rows(&s, X, plan, b->Xp, stream));
+  ETR_TRY(etr_expert_ffn(c, &route, b->Xp, W1g, W1u, W2, b->G, b->U, b->H, b->O, b->stats, b->ws, stream));
+  return etr_unsort_rows(&s, b->O, weights, plan, Y, stream);
+}
+
+etr_status etr_routed_backward(const etr_config* c, const float* weights, const void* W1g, const void* W1u, const void* W2, const void* dY,
+                               const etr_buffers* b, const etr_sort_plan* plan, void* dX, float* dweights, void* dW1g, void* dW1u,
+                               void* dW2, void* stream) {
+  ETR_TRY(etr_validate(c));
+  etr_route route;
+  ETR_TRY(routed_route(b, plan, &route));
+  ETR_TRY(check_ptrs({weights, W1g, W1u, W2, dY, b->stats, b->dO, b->Xp, b->G, b->U, b->H, b->O, b->dG, b->dU, b->dXp, b->ws, dX, dweights,
+                      dW1g, dW1u, dW2}));
+  ETR_TRY(check_workspace(c, b, false, false));
+  const etr_sort_config s = routed_sort_config(c);
+  ETR_TRY(etr_unsort_rows_bwd(&s, dY, b->O, weights, plan, b->dO, dweights, stream));
+  ETR_TRY(expert_ffn_bwd(c, &route, b->dO, b->Xp, b->G, b->U, b->H, W1g, W1u, W2, b->dG, b->dU, b->dXp, dW1g, dW1u, dW2, b->stats, b->ws,
+                         false, stream));
+  return etr_sort_rows_bwd(&s, b->dXp, plan, dX, stream);
+}
+
+// ---- norm, layer, join ------------------------------------------------------------------------------
+etr_status etr_block_bind(const etr_norm_config* n, void* base, size_t bytes, etr_block_buffers* out, size_t* need) {
+  size_t ws = 0;
+  ETR_TRY(etr_norm_workspace_bytes(n, &ws));
+  if (need == nullptr && out == nullptr) return ETR_ERR_ARG;
+  if (out && base == nullptr) return ETR_ERR_ARG;
+  if (out && (reinterpret_cast<uintptr_t>(base) & 255u)) return ETR_ERR_ALIGN;
+  const size_t rows = (size_t)n->T * n->d * elem_bytes(n->dtype);
+  Carver cv{(char*)base, 0};
+  etr_block_buffers b;
+  b.N = cv.take(rows); b.Y = cv.take(rows); b.dN = cv.take(rows); b.dY = cv.take(rows);
+  b.rstd_x = (float*)cv.take((size_t)n->T * 4);
+  b.rstd_y = (float*)cv.take((size_t)n->T * 4);
+  b.ws = cv.take(ws);
+  if (need) *need = align_up(cv.off, 256);
+  if (out) {
+    if (bytes < cv.off) return ETR_ERR_WORKSPACE;
+    *out = b;
+  }
+  return ETR_OK;
+}
+
+static etr_status block_check(const etr_config* c, const etr_norm_config* n, const etr_buffers* b, const etr_block_buffers* bb) {
+  ETR_TRY(etr_validate(c));
+  ETR_TRY(etr_norm_validate(n));
+  if (n->T != c->T || n->d != c->d || n->dtype != c->dtype) return ETR_ERR_SHAPE;
+  if (b == nullptr || bb == nullptr) return ETR_ERR_ARG;
+  return check_ptrs({bb->N, bb->Y, bb->rstd_x, bb->rstd_y});
+}
+
+etr_status etr_block_forward(const etr_config* c, const etr_norm_config* n, const void* X, const float* w_pre, const float* w_post,
+                             const float* gate, const float* R, const void* W1g, const void* W1u, const void* W2, const etr_buffers* b,
+                             const etr_block_buffers* bb, void* Xo, void* stream) {
+  ETR_TRY(block_check(c, n, b, bb));
+  ETR_TRY(check_ptrs({X, Xo, R, W1g, W1u, W2}));
+  if (!aligned16(w_pre) || !aligned16(w_post) || !aligned16(gate)) return ETR_ERR_ALIGN;
+  ETR_TRY(check_workspace(c, b, true, false));
+  ETR_TRY(etr_prenorm(n, X, w_pre, bb->N, bb->rstd_x, stream));
+  ETR_TRY(etr_layer_forward(c, bb->N, R, W1g, W1u, W2, b, bb->Y, stream));
+  return etr_join(n, X, bb->Y, w_post, gate, nullptr, Xo, nullptr, bb->rstd_y, nullptr, stream);
+}
+
+etr_status etr_block_backward(const etr_config* c, const etr_norm_config* n, const void* X, const float* w_pre, const float* w_post,
+                              const float* gate, const float* R, const void* W1g, const void* W1u, const void* W2, const void* dXo,
+                              const etr_buffers* b, const etr_block_buffers* bb, void* dX, float* dw_pre, float* dw_post, float* dgate,
+                              float* dR, void* dW1g, void* dW1u, void* dW2, void* stream) {
+  ETR_TRY(block_check(c, n, b, bb));
+  ETR_TRY(check_ptrs({X, dXo, dX, R, W1g, W1u, W2, dR, dW1g, dW1u, dW2, bb->dN, bb->dY, bb->ws}));
+  for (const void* p : {(const void*)w_pre, (const void*)w_post, (const void*)gate, (const void*)dw_pre, (const void*)dw_post, (const void*)dgate})
+    if (!aligned16(p)) return ETR_ERR_ALIGN;
+  ETR_TRY(check_workspace(c, b, false, true));
+  ETR_TRY(etr_join_bwd(n, dXo, nullptr, bb->Y, nullptr, w_post, gate, nullptr, bb->rstd_y, nullptr, dX, bb->dY, dw_post, dgate, nullptr,
+                       bb->ws, stream));
+  ETR_TRY(etr_layer_backward(c, bb->N, R, W1g, W1u, W2, bb->dY, b, bb->dN, dR, dW1g, dW1u, dW2, stream));
+  return etr_prenorm_bwd(n, bb->dN, X, w_pre, bb->rstd_x, dX, dX, dw_pre, bb->ws, stream);
+}
+
 // Side streams and events for the host-buffer step (host-side objects, created once per device).
 struct HostSlotEvents { cudaEvent_t x_ready, dy_ready, fwd_done, bwd_done, y_down, dx_down; bool used; };
 struct HostStepCtx {

@@ -32,6 +32,7 @@ EXPORTS = [
     "etr_launch_count", "etr_timing_enable", "etr_timing_collect",
     "etr_sort_validate", "etr_sort_n_rows", "etr_sort_plan_bind", "etr_sort", "etr_sort_rows", "etr_sort_rows_bwd",
     "etr_unsort_rows", "etr_unsort_rows_bwd",
+    "etr_routed_forward", "etr_routed_backward", "etr_block_bind", "etr_block_forward", "etr_block_backward",
     "etr_norm_validate", "etr_norm_workspace_bytes", "etr_prenorm", "etr_prenorm_bwd", "etr_join", "etr_join_bwd",
 ]
 
@@ -96,7 +97,7 @@ def lib():
         l.etr_launch_count.restype = C.c_int64
         l.etr_c_stride.restype = C.c_int32
         l.etr_sort_n_rows.restype = C.c_int64
-        l.etr_sort_plan_bind.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        l.etr_sort_plan_bind.argtypes = l.etr_block_bind.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         _lib = l
     return _lib
 
@@ -510,3 +511,54 @@ def join(cfg, X, Y, w_post, gate, w_next, Xo, N, rstd_y=None, rstd_o=None):
 
 def join_bwd(cfg, dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws):
     _row_op(8, C.addressof(cfg), -1, dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws)
+
+
+# ---- the layer's experts under a given choice; norm, layer and join as one call --------------------------
+def routed_sort_config(cfg: Config) -> SortConfig:
+    """Configuration of the plan (SortBuffers) that routed_forward and routed_backward take."""
+    return make_sort_config(T=cfg.T, k=cfg.k, E=cfg.E, d=cfg.d, dtype=cfg.dtype, align=128, capacity=cfg.capacity)
+
+
+def routed_forward(cfg, X, topk_idx, weights, W1g, W1u, W2, buf: LayerBuffers, plan: SortBuffers, Y):
+    _check(lib().etr_routed_forward(C.byref(cfg), _p(X), _p(topk_idx), _p(weights), _p(W1g), _p(W1u), _p(W2),
+                                    C.byref(buf.c), C.byref(plan.c), _p(Y), _stream()), "etr_routed_forward")
+
+
+def routed_backward(cfg, weights, W1g, W1u, W2, dY, buf: LayerBuffers, plan: SortBuffers, dX, dweights, dW1g, dW1u, dW2):
+    _check(lib().etr_routed_backward(C.byref(cfg), _p(weights), _p(W1g), _p(W1u), _p(W2), _p(dY), C.byref(buf.c),
+                                     C.byref(plan.c), _p(dX), _p(dweights), _p(dW1g), _p(dW1u), _p(dW2), _stream()),
+           "etr_routed_backward")
+
+
+class BlockBuffersC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("N", "Y", "dN", "dY", "rstd_x", "rstd_y", "ws")]
+
+
+class BlockBuffers:
+    """What a block keeps besides the layer's buffers: one device block carved by etr_block_bind."""
+
+    def __init__(self, ncfg: NormConfig, device="cuda"):
+        n = C.c_size_t(0)
+        _check(lib().etr_block_bind(C.byref(ncfg), None, C.c_size_t(0), None, C.byref(n)), "etr_block_bind")
+        self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
+        base = (self.block.data_ptr() + 255) // 256 * 256
+        self.c = BlockBuffersC()
+        _check(lib().etr_block_bind(C.byref(ncfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_block_bind")
+        act, rows = torch_dtype(ncfg), (ncfg.T, ncfg.d)
+        for name in ("N", "Y", "dN", "dY"):
+            off = getattr(self.c, name) - self.block.data_ptr()
+            size = ncfg.T * ncfg.d * torch.empty((), dtype=act).element_size()
+            setattr(self, name, self.block[off:off + size].view(act).view(rows))
+
+
+def block_forward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, buf: LayerBuffers, bb: BlockBuffers, Xo):
+    _check(lib().etr_block_forward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
+                                   _p(W1u), _p(W2), C.byref(buf.c), C.byref(bb.c), _p(Xo), _stream()), "etr_block_forward")
+
+
+def block_backward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, dXo, buf: LayerBuffers, bb: BlockBuffers, dX, dw_pre,
+                   dw_post, dgate, dR, dW1g, dW1u, dW2):
+    _check(lib().etr_block_backward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
+                                    _p(W1u), _p(W2), _p(dXo), C.byref(buf.c), C.byref(bb.c), _p(dX), _p(dw_pre),
+                                    _p(dw_post), _p(dgate), _p(dR), _p(dW1g), _p(dW1u), _p(dW2), _stream()),
+           "etr_block_backward")

@@ -219,3 +219,60 @@ def test_binding_refuses_what_addresses_do_not_show():
     with pytest.raises(etr.EtrError) as e:
         etr.sort(plan.cfg, torch.zeros(4, 2, dtype=torch.int32), plan)
     assert e.value.code == etr.ERR_ARG
+
+
+def composed(cfg, ncfg):
+    """The four composed calls with addresses that nothing is read from; a change replaces one argument by name."""
+    L, ok = etr.lib(), 1 << 20
+    p = C.c_void_p(ok)
+    buf, n = etr.Buffers(), C.c_size_t(0)
+    assert L.etr_buffers_bytes(C.byref(cfg), 0, C.byref(n)) == etr.OK
+    assert L.etr_buffers_bind(C.byref(cfg), 0, p, n, C.byref(buf)) == etr.OK
+    a = dict(cfg=C.byref(cfg), ncfg=C.byref(ncfg), buf=C.byref(buf), plan=C.byref(etr.SortPlan(*[ok] * 6)),
+             bb=C.byref(etr.BlockBuffersC(*[ok] * 7)), stream=None)
+    names = {"etr_routed_forward": "cfg X ids weights W1g W1u W2 buf plan Y stream",
+             "etr_routed_backward": "cfg weights W1g W1u W2 dY buf plan dX dweights dW1g dW1u dW2 stream",
+             "etr_block_forward": "cfg ncfg X w_pre? w_post? gate? R W1g W1u W2 buf bb Xo stream",
+             "etr_block_backward": "cfg ncfg X w_pre? w_post? gate? R W1g W1u W2 dXo buf bb dX dw_pre? dw_post? dgate? dR dW1g dW1u dW2 stream"}
+
+    def call(name, **change):
+        return getattr(L, name)(*[change.get(x.rstrip("?"), a.get(x, p)) for x in names[name].split()])
+
+    return names, call, buf
+
+
+def test_composed_calls_check_their_arguments():
+    cfg = etr.make_config(T=64, d=256, D=8, E=8, k=2, h=128, capacity=64, dtype=etr.BF16, weight_dtype=etr.F32)
+    ncfg = etr.make_norm_config(T=64, d=256, dtype=etr.BF16)
+    names, call, buf = composed(cfg, ncfg)
+    for name, args in names.items():
+        for x in args.split():
+            if x in ("cfg", "ncfg", "buf", "plan", "bb", "stream"):
+                if x != "stream":
+                    assert call(name, **{x: None}) == etr.ERR_ARG, (name, x)
+                continue
+            assert call(name, **{x.rstrip("?"): C.c_void_p((1 << 20) + 4)}) == etr.ERR_ALIGN, (name, x)
+            if not x.endswith("?"):
+                assert call(name, **{x: None}) == etr.ERR_ARG, (name, x)
+        small = etr.Buffers.from_buffer_copy(buf)
+        small.ws_bytes = 16
+        assert call(name, buf=C.byref(small)) == etr.ERR_WORKSPACE
+        if name.startswith("etr_block"):
+            for bad in (dict(T=63), dict(d=248), dict(dtype=etr.F32)):
+                other = etr.make_norm_config(**dict(dict(T=64, d=256, dtype=etr.BF16), **bad))
+                assert call(name, ncfg=C.byref(other)) == etr.ERR_SHAPE
+    many = etr.make_config(T=64, d=512, D=8, E=64, k=33, h=128, capacity=64, dtype=etr.BF16)
+    assert etr.validate(many) == etr.OK
+    for name in ("etr_routed_forward", "etr_routed_backward"):
+        assert composed(many, ncfg)[1](name) == etr.ERR_SHAPE
+
+
+def test_block_buffers_are_carved_in_order():
+    ncfg, L, n, b = etr.make_norm_config(T=65, d=264, dtype=etr.BF16), etr.lib(), C.c_size_t(0), etr.BlockBuffersC()
+    assert L.etr_block_bind(C.byref(ncfg), None, 0, None, C.byref(n)) == etr.OK and n.value % 256 == 0
+    assert L.etr_block_bind(C.byref(ncfg), C.c_void_p((1 << 20) + 16), n, C.byref(b), None) == etr.ERR_ALIGN
+    assert L.etr_block_bind(C.byref(ncfg), C.c_void_p(1 << 20), C.c_size_t(4096), C.byref(b), None) == etr.ERR_WORKSPACE
+    assert L.etr_block_bind(C.byref(ncfg), C.c_void_p(1 << 20), n, C.byref(b), None) == etr.OK
+    rows = 65 * 264 * 2
+    at = [getattr(b, x) for x in ("N", "Y", "dN", "dY", "rstd_x", "rstd_y", "ws")] + [(1 << 20) + n.value]
+    assert all(v % 256 == 0 for v in at) and all(q - p >= s for p, q, s in zip(at, at[1:], [rows] * 4 + [260] * 2 + [etr.norm_workspace_bytes(ncfg)]))
