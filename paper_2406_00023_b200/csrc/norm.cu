@@ -143,14 +143,16 @@ struct RowRing {
   __device__ __forceinline__ void next() { stage = stage + 1 < stages ? stage + 1 : 0; }
 };
 
-// Forward: at most 80 registers a thread, so that 768 threads fit an SM; backward: 128 and 512.
-constexpr int NORM_FWD_REGS = 80, NORM_FWD_THREADS = 768, NORM_BWD_REGS = 128, NORM_BWD_THREADS = 512;
+// Threads of an SM: forward 768 with at most 80 registers each, backward 512 with 128 (which is what the launch bounds ask for;
+// a block has at most 512).
+constexpr int NORM_FWD_THREADS = 768, NORM_BWD_THREADS = 512;
 
 // Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.
 template <class T, int NV, bool RING, bool JOIN>
-__global__ void __maxnreg__(NV > 2 ? 128 : NORM_FWD_REGS)
+__global__ void __launch_bounds__(NV > 2 ? 512 : NORM_FWD_THREADS)
 norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 2 : 1, XX = 0, YY = NT - 1;
+  grid_sync();
   extern __shared__ uint4 ring_smem[];
   __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
   const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
@@ -176,7 +178,6 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
     ring.commit();
   };
   row_sum.init();
-  grid_sync();
   long long tile = (long long)blockIdx.x * sh.rpb;
   size_t at = (size_t)(tile + row) * np + tg, ahead = at;
   if (RING)
@@ -251,10 +252,11 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
 //   s1 = <w_next dN, x>,  G = dXo + r_o w_next dN - (r_o^2 (r_o s1 / d)) x,   s2 = <w_post G, y>,  dgate = b r_y s2,
 //   dY = (b gate r_y) w_post G - (b gate r_y (r_y (r_y s2 / d))) y
 template <class T, int NV, bool RING, bool JOIN>
-__global__ void __maxnreg__(NORM_BWD_REGS)
+__global__ void __launch_bounds__(NORM_BWD_THREADS)
 norm_bwd_kernel(const NormArgs p, const RowShape sh) {
   constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 4 : 3;
   enum { DN, XO, DXO, YY };
+  grid_sync();
   extern __shared__ uint4 ring_smem[];
   __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
   const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
@@ -284,7 +286,6 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
     ring.commit();
   };
   row_sum.init();
-  grid_sync();
   long long tile = (long long)blockIdx.x * sh.rpb;
   size_t at = (size_t)(tile + row) * np + tg, ahead = at;
   if (RING)

@@ -25,6 +25,7 @@ struct SortShape {
 // sort_plan_kernel.
 __global__ void __launch_bounds__(SORT_WARPS * 32)
 sort_count_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ part) {
+  grid_sync();
   extern __shared__ int mine[];                  // [E]
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -32,7 +33,6 @@ sort_count_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ part) {
   const long long beg = (long long)blockIdx.x * per, end = min((long long)s.N, beg + per);
   for (int e = tid; e < s.E; e += threads) mine[e] = 0;
   __syncthreads();
-  grid_sync();
 #pragma unroll 4
   for (long long i = beg + tid; i < end; i += threads) {
     const int e = ids[i];
@@ -57,6 +57,7 @@ __global__ void __launch_bounds__(SORT_WARPS * 32)
 sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclusters, int32_t* __restrict__ counts,
                  int32_t* __restrict__ offsets, int32_t* __restrict__ totals, int32_t* __restrict__ row_token,
                  int32_t* __restrict__ pos) {
+  grid_sync();
   extern __shared__ int sm[];
   cg::cluster_group cluster = cg::this_cluster();
   const int threads = blockDim.x, warps = threads >> 5, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -71,7 +72,6 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   const int n = (int)max(0ll, min((long long)s.run, (long long)s.N - beg));
   int* cnt = wc + warp * s.E;
   __syncthreads();
-  grid_sync();
 #pragma unroll 4
   for (int i = lane; i < n; i += 32) {
     const int e = ids[beg + i];
