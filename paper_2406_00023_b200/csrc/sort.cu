@@ -14,7 +14,7 @@ constexpr int SORT_WARPS = 16;                   // at most
 constexpr int SORT_CLUSTER = 8;
 constexpr int SORT_MAX_CLUSTERS = 18;            // 144 of the 148 SMs
 constexpr int SORT_ONE_CLUSTER = 32768;          // pairs that one cluster takes without a counting launch before it
-constexpr int SORT_RUN = 64;                     // pairs per warp that are worth another CTA
+constexpr int SORT_RUN = 32;                     // pairs per warp that are worth another CTA
 
 struct SortShape {
   int N, k, E, align, capacity, stride, n_rows;      // stride: rows between experts in the capacity form, else 0
@@ -52,7 +52,9 @@ sort_count_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ part) {
 // prefix sums within the CTA, through distributed shared memory across the cluster, and through `part` across the
 // clusters (nclusters > 1).  The row of a pair is then its expert's start, plus the pairs of earlier warps, plus those
 // before it in its own warp (one match over the warp's 32 ids a round).  No atomics decide an order, so the plan is
-// stable and the same every time.  Bound by the latency of that chain: a short batch is one launch of one small CTA.
+// stable and the same every time.  Bound by the latency of that chain, so a run's first SORT_KEPT rounds of ids stay in
+// registers, loops over warps and CTAs are unrolled (their loads in flight together), and a short batch is one small CTA.
+constexpr int SORT_KEPT = 4;
 __global__ void __launch_bounds__(SORT_WARPS * 32)
 sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclusters, int32_t* __restrict__ counts,
                  int32_t* __restrict__ offsets, int32_t* __restrict__ totals, int32_t* __restrict__ row_token,
@@ -65,23 +67,35 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   int* wc = sm;                                  // [warps][E] pairs of this warp, then of the warps before it
   int* mine = wc + warps * s.E;                  // [E] pairs of this CTA
   int* start = mine + s.E;                       // [E] first row of the expert
-  int* kept = start + s.E;                       // [E]
+  int* before = start + s.E;                     // [E] pairs in the CTAs before this one
+  int* used = before + s.E;                      // [E] pairs that get a row
   __shared__ int s_rows[SORT_WARPS], s_found[SORT_WARPS], s_kept[SORT_WARPS];
-  for (int i = tid; i < warps * s.E; i += threads) wc[i] = 0;
   const long long beg = ((long long)blockIdx.x * warps + warp) * s.run;
   const int n = (int)max(0ll, min((long long)s.run, (long long)s.N - beg));
+  int id[SORT_KEPT];
+#pragma unroll
+  for (int u = 0; u < SORT_KEPT; ++u) id[u] = 32 * u + lane < n ? ids[beg + 32 * u + lane] : -1;
+  for (int i = tid; i < warps * s.E; i += threads) wc[i] = 0;
   int* cnt = wc + warp * s.E;
   __syncthreads();
+#pragma unroll
+  for (int u = 0; u < SORT_KEPT; ++u)
+    if ((unsigned)id[u] < (unsigned)s.E) atomicAdd(&cnt[id[u]], 1);
 #pragma unroll 4
-  for (int i = lane; i < n; i += 32) {
+  for (int i = 32 * SORT_KEPT + lane; i < n; i += 32) {
     const int e = ids[beg + i];
     if ((unsigned)e < (unsigned)s.E) atomicAdd(&cnt[e], 1);
   }
   __syncthreads();
   for (int e = tid; e < s.E; e += threads) {
-    int acc = 0;
-#pragma unroll 4
-    for (int w = 0; w < warps; ++w) { const int c = wc[w * s.E + e]; wc[w * s.E + e] = acc; acc += c; }
+    int c[SORT_WARPS], acc = 0;
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) c[w] = w < warps ? wc[w * s.E + e] : 0;
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) {
+      if (w < warps) wc[w * s.E + e] = acc;
+      acc += c[w];
+    }
     mine[e] = acc;
   }
   if (ncta > 1) cluster.sync(); else __syncthreads();
@@ -91,30 +105,35 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   for (int u = 0; u < 2; ++u) {
     const int e = 2 * tid + u;
     if (e >= s.E) break;
-    int all = 0, before = 0;
-    for (int c = 0; c < ncta; ++c) {
-      const int v = cluster.map_shared_rank(mine, c)[e];
-      all += v;
-      before += c < rank ? v : 0;
+    int all = 0, ahead = 0;
+    if (ncta == 1) {
+      all = mine[e];
+    } else {
+#pragma unroll
+      for (int c = 0; c < SORT_CLUSTER; ++c) {
+        const int v = c < ncta ? cluster.map_shared_rank(mine, c)[e] : 0;
+        all += v;
+        ahead += c < rank ? v : 0;
+      }
     }
     if (nclusters > 1) {
       all = 0;
-#pragma unroll 6
-      for (int c = 0; c < nclusters; ++c) {
-        const int v = part[(size_t)c * s.E + e];
+#pragma unroll
+      for (int c = 0; c < SORT_MAX_CLUSTERS; ++c) {
+        const int v = c < nclusters ? part[(size_t)c * s.E + e] : 0;
         all += v;
-        before += c < my_cluster ? v : 0;
+        ahead += c < my_cluster ? v : 0;
       }
     }
     const int keep = s.capacity ? min(all, s.capacity) : all;
-    if (before)
-      for (int w = 0; w < warps; ++w) wc[w * s.E + e] += before;
-    kept[e] = keep;
+    before[e] = ahead;
+    used[e] = keep;
     found += all;
     keeps += keep;
     rows[u] = s.capacity ? s.stride : (keep + s.align - 1) / s.align * s.align;
     if (blockIdx.x == 0) counts[e] = keep;
   }
+  if (ncta > 1) cluster.barrier_arrive();        // done with the other CTAs' counts; waited for before leaving
   int inc = rows[0] + rows[1];
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -128,14 +147,9 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   }
   if (lane == 31) { s_rows[warp] = inc; s_found[warp] = found; s_kept[warp] = keeps; }
   __syncthreads();
-  int at = inc - rows[0] - rows[1], end = 0;
-  found = keeps = 0;
-  for (int w = 0; w < warps; ++w) {
-    at += w < warp ? s_rows[w] : 0;
-    end += s_rows[w];
-    found += s_found[w];
-    keeps += s_kept[w];
-  }
+  int at = inc - rows[0] - rows[1];
+#pragma unroll
+  for (int w = 0; w < SORT_WARPS; ++w) at += w < warp ? s_rows[w] : 0;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int e = 2 * tid + u;
@@ -145,21 +159,18 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     }
     at += rows[u];
   }
-  if (blockIdx.x == 0 && tid == 0) {
-    offsets[s.E] = end;
-    totals[0] = keeps; totals[1] = found - keeps; totals[2] = s.N - found; totals[3] = 0;
-  }
   __syncthreads();
   const int limit = s.capacity ? s.capacity : s.N;
-  for (int i0 = 0; i0 < n; i0 += 128) {          // four rounds' ids are asked for at once
-    int id[4];
+  for (int i0 = 0; i0 < n; i0 += 32 * SORT_KEPT) {
+    if (i0 > 0) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = i0 + 32 * u + lane;
-      id[u] = i < n ? ids[beg + i] : -1;
+      for (int u = 0; u < SORT_KEPT; ++u) {
+        const int i = i0 + 32 * u + lane;
+        id[u] = i < n ? ids[beg + i] : -1;
+      }
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < SORT_KEPT; ++u) {
       const int i = i0 + 32 * u + lane, e = id[u];
       if (i0 + 32 * u >= n) break;
       const bool ok = (unsigned)e < (unsigned)s.E;
@@ -170,18 +181,34 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
       if (ok && (same >> lane) == 1u) cnt[e] = r + 1;         // the last of its kind in this round
       __syncwarp();
       if (i < n) {
+        if (ok) r += before[e];
         const int row = ok && r < limit ? start[e] + r : -1;
         pos[beg + i] = row;
         if (row >= 0) row_token[row] = (int)((beg + i) / s.k);
       }
     }
   }
-  // rows without a token
-  for (int e = blockIdx.x; e < s.E; e += gridDim.x) {
-    const int stop = e + 1 < s.E ? start[e + 1] : s.n_rows;
-    for (int r = start[e] + kept[e] + tid; r < stop; r += threads) row_token[r] = -1;
+  // Rows without a token, an expert's at a time by one warp, or by several where there are more warps than experts; without
+  // gaps between experts only those behind the last.
+  const bool gaps = s.align > 1;
+  const int first = gaps ? 0 : s.E - 1, spans = s.E - first, all_warps = gridDim.x * warps, parts = max(1, all_warps / spans);
+  for (int x = blockIdx.x * warps + warp; x < spans * parts; x += all_warps) {
+    const int e = first + x % spans, part = x / spans;
+    const int lo = start[e] + used[e], hi = e + 1 < s.E ? start[e + 1] : s.n_rows;
+    const int lo4 = min((lo + 3) & ~3, hi), hi4 = max(hi & ~3, lo4);
+    if (part == 0) {
+      if (lo + lane < lo4) row_token[lo + lane] = -1;
+      if (hi4 + lane < hi) row_token[hi4 + lane] = -1;
+    }
+    for (int r = lo4 + 4 * (lane + 32 * part); r < hi4; r += 128 * parts) *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
   }
-  if (ncta > 1) cluster.sync();                  // no CTA leaves while another may still read its counts
+  if (blockIdx.x == 0 && tid == 0) {
+    int end = 0, all = 0, with = 0;
+    for (int w = 0; w < warps; ++w) { end += s_rows[w]; all += s_found[w]; with += s_kept[w]; }
+    offsets[s.E] = end;
+    totals[0] = with; totals[1] = all - with; totals[2] = s.N - all; totals[3] = 0;
+  }
+  if (ncta > 1) cluster.barrier_wait();          // no CTA leaves while another may still read its counts
 }
 
 // Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first PAD_SHARES * E blocks of a
@@ -347,7 +374,7 @@ static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD
 // pairs 13.9 us in one cluster, 16.6 with the count; 65536 17.2 and 16.3; 131072 26.5 and 19.8; 524288 94 and 41.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
-  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 3) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 4) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
   SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c), 0};
   const int cta = SORT_WARPS * SORT_RUN, cluster = cta * SORT_CLUSTER;
   int warps = SORT_WARPS, ncta = 1, nclusters = 1;
@@ -365,7 +392,7 @@ static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, cons
     launch_kernel(sort_count_kernel, nclusters * SORT_CLUSTER, SORT_WARPS * 32, (size_t)c->E * 4, st, SORT_CLUSTER, ids, s, p->scratch);
     ETR_LAUNCH_CHECK();
   }
-  const size_t smem = (size_t)(warps + 3) * c->E * 4;
+  const size_t smem = (size_t)(warps + 4) * c->E * 4;
   ETR_TIME_BEGIN("sort_plan_kernel");
   launch_kernel(sort_plan_kernel, nclusters * ncta, warps * 32, smem, st, ncta, ids, s, (const int32_t*)p->scratch, nclusters, p->counts,
                 p->offsets, p->totals, p->row_token, p->pos);
