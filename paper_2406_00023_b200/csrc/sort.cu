@@ -11,7 +11,8 @@ namespace cg = cooperative_groups;
 namespace etr {
 
 constexpr int SORT_WARPS = 16;                   // at most
-constexpr int SORT_CLUSTER = 8;
+constexpr int SORT_CLUSTER = 8;                   // CTAs of a cluster, where there are several
+constexpr int SORT_ALONE = 16;                    // CTAs at most of one that works alone
 constexpr int SORT_MAX_CLUSTERS = 18;            // 144 of the 148 SMs
 constexpr int SORT_ONE_CLUSTER = 32768;          // pairs that one cluster takes without a counting launch before it
 constexpr int SORT_RUN = 32;                     // pairs per warp that are worth another CTA
@@ -109,12 +110,13 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     if (ncta == 1) {
       all = mine[e];
     } else {
+      for (int c0 = 0; c0 < ncta; c0 += 8)
 #pragma unroll
-      for (int c = 0; c < SORT_CLUSTER; ++c) {
-        const int v = c < ncta ? cluster.map_shared_rank(mine, c)[e] : 0;
-        all += v;
-        ahead += c < rank ? v : 0;
-      }
+        for (int c = 0; c < 8; ++c) {
+          const int v = c0 + c < ncta ? cluster.map_shared_rank(mine, c0 + c)[e] : 0;
+          all += v;
+          ahead += c0 + c < rank ? v : 0;
+        }
     }
     if (nclusters > 1) {
       all = 0;
@@ -367,23 +369,38 @@ static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* 
   return ETR_OK;
 }
 
+// Clusters of more than 8 CTAs are allowed per kernel and device.
+template <class K>
+static bool ensure_wide_cluster(K kernel, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_acquire) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_release);
+  return true;
+}
+
 static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD_SHARES * c->E : 0; }
 
-// One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 8 of 16 warps; longer batches take up to 18 such
-// clusters, and a launch before that counts the clusters' pairs.  Measured with the rows of d = 64 behind it: 32768
-// pairs 13.9 us in one cluster, 16.6 with the count; 65536 17.2 and 16.3; 131072 26.5 and 19.8; 524288 94 and 41.
+// One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 16 of 16 warps (an opt-in size); longer batches take up to
+// 18 clusters of 8, and a launch before that counts the clusters' pairs.  Measured, a plan by itself: 32768 pairs of 32
+// experts 6.4 us in one cluster of 16, 8.4 of 8, 10 with the count; 131072 of 64 10.3 us with the count, 14.4 without.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
-  static std::atomic<unsigned long long> done{0};
+  static std::atomic<unsigned long long> done{0}, wide{0};
   if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 4) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  if (!ensure_wide_cluster(sort_plan_kernel, wide)) return ETR_ERR_CUDA;
   SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c), 0};
-  const int cta = SORT_WARPS * SORT_RUN, cluster = cta * SORT_CLUSTER;
+  const int cta = SORT_WARPS * SORT_RUN;
   int warps = SORT_WARPS, ncta = 1, nclusters = 1;
   if (s.N <= cta) {
     warps = std::max(std::max(ceil_div(s.N, 32), ceil_div(s.E, 64)), 4);
     warps = std::min(warps, SORT_WARPS);
+  } else if (s.N <= SORT_ONE_CLUSTER) {
+    while (ncta < SORT_ALONE && s.N > ncta * cta) ncta *= 2;
   } else {
-    while (ncta < SORT_CLUSTER && s.N > ncta * cta) ncta *= 2;
-    if (s.N > SORT_ONE_CLUSTER) nclusters = std::min((s.N + cluster - 1) / cluster, SORT_MAX_CLUSTERS);
+    ncta = SORT_CLUSTER;
+    nclusters = std::min(s.N / (cta * SORT_CLUSTER) + 1, SORT_MAX_CLUSTERS);
   }
   const int all = warps * ncta * nclusters;
   s.run = ((s.N + all - 1) / all + 31) & ~31;
