@@ -420,24 +420,24 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
   }
 }
 
-// dw[c] = sum over the blocks' partial rows, in a fixed order; grid y: which weight.
-__global__ void __launch_bounds__(256)
+// dw[c] = sum over the blocks' partial rows, in a fixed order; grid y: which weight.  32 columns a block, every warp a 32nd of the
+// rows (some ten of them, their loads in flight together).
+__global__ void __launch_bounds__(1024)
 norm_dw_kernel(const float* part0, const float* part1, float* __restrict__ dw0, float* __restrict__ dw1, int rows, int d) {
-  __shared__ float red[8][33];
   grid_sync();
+  __shared__ float red[32][33];
   const float* part = blockIdx.y ? part1 : part0;
   float* dw = blockIdx.y ? dw1 : dw0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < d)
-    for (int r = warp; r < rows; r += 8) s += part[(size_t)r * d + c];
+  if (c < d) {
+#pragma unroll 8
+    for (int r = warp; r < rows; r += 32) s += part[(size_t)r * d + c];
+  }
   red[warp][lane] = s;
   __syncthreads();
-  if (warp == 0 && c < d) {
-#pragma unroll
-    for (int w = 1; w < 8; ++w) s += red[w][lane];
-    dw[c] = s;
-  }
+  s = warp_sum(red[lane][warp]);                 // column `warp`, by one warp
+  if (lane == 0 && blockIdx.x * 32 + warp < d) dw[blockIdx.x * 32 + warp] = s;
 }
 
 // ---- launches ----------------------------------------------------------------------------------
@@ -555,7 +555,7 @@ static etr_status norm_dw(const etr_norm_config* c, const NormArgs& p, float* dw
   const bool both = dw_next && dw_post;
   const float* a = dw_next ? p.part_next : p.part_post;
   ETR_TIME_BEGIN("norm_dw_kernel");
-  launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 256, 0, st, 1, a, (const float*)p.part_post, dw_next ? dw_next : dw_post,
+  launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 1024, 0, st, 1, a, (const float*)p.part_post, dw_next ? dw_next : dw_post,
                 dw_post, norm_bwd_blocks(c->T, c->d, c->dtype), c->d);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
