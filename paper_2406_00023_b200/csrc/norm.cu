@@ -21,7 +21,7 @@ struct NormArgs {
 
 // How rows lie on a block's threads: tpr threads hold a row (a power of two up to 32, or whole warps), NV pieces of 16 bytes each
 // (piece u of a thread is piece tg + u tpr of the row), rpb rows side by side in a block.
-struct RowShape { int tpr, rpb, stages; };
+struct RowShape { int tpr, rpb; };
 
 // Sum over a row's threads, in every one of them.  Two arrays take turns from sum to sum, so that one barrier a sum is
 // enough: whoever writes an array again has passed the barrier of the sum between, and so has every reader.
@@ -112,25 +112,23 @@ __device__ __forceinline__ void load_gain(const float* w, int col, float2* out) 
   }
 }
 
-// The rows of up to NT tensors, tiles ahead of their use.  A thread copies (cp.async) exactly the pieces that it reads
+// The rows of up to NT tensors, one tile ahead of their use.  A thread copies (cp.async) exactly the pieces that it reads
 // itself, so that a wait for its own copies is all the synchronisation the ring needs.  Pieces behind a row's end and rows
-// behind the last arrive as zeros (a copy of no bytes).  RING false: rows so long that two tiles do not fit come straight
-// from global memory.
+// behind the last arrive as zeros (a copy of no bytes).  A second tile ahead cost time (bf16: prenorm of 65536 x 4096 167 us
+// with one, 188 with two; join backward of 16384 x 4096 137 and 145).  RING false: rows so long that two tiles do not
+// fit shared memory come straight from global memory.
 template <int NT, int NV, bool RING>
 struct RowRing {
   uint32_t smem;                                  // this thread's first slot
   uint32_t pitch;                                 // between pieces, 16 bytes a thread
-  int stages, stage;
+  int stage;
   __device__ __forceinline__ uint32_t slot(int st, int tensor, int u) const { return smem + ((st * NT + tensor) * NV + u) * pitch; }
   __device__ __forceinline__ void fetch(int st, int tensor, int u, const uint4* src, bool there) const {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(slot(st, tensor, u)), "l"(src), "r"(there ? 16 : 0) : "memory");
   }
   __device__ __forceinline__ void commit() const { asm volatile("cp.async.commit_group;" ::: "memory"); }
-  // all copies but those of the stages - 1 youngest tiles have arrived
-  __device__ __forceinline__ void wait() const {
-    if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-    else asm volatile("cp.async.wait_group 1;" ::: "memory");
-  }
+  // all copies but those of the youngest tile have arrived
+  __device__ __forceinline__ void wait() const { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
   __device__ __forceinline__ uint4 piece(int tensor, int u, const void* base, size_t at, bool there) const {
     if (RING) {
       uint4 q;
@@ -139,13 +137,13 @@ struct RowRing {
     }
     return there ? ((const uint4*)base)[at] : make_uint4(0, 0, 0, 0);
   }
-  __device__ __forceinline__ int oldest() const { return stage == 0 ? stages - 1 : stage - 1; }       // free for a new tile
-  __device__ __forceinline__ void next() { stage = stage + 1 < stages ? stage + 1 : 0; }
 };
 
-// Threads of an SM: forward 768 with at most 80 registers each, backward 512 with 128 (which is what the launch bounds ask for;
-// a block has at most 512).
-constexpr int NORM_FWD_THREADS = 768, NORM_BWD_THREADS = 512;
+// Threads of an SM, which is what the launch bounds ask for (a block has at most 512): forward 768 with at most 80 registers each;
+// prenorm's backward 576 with 112, which fits a third block of 192 threads (20000 x 1088: 49 % of the copy rate with two, 76
+// with three); the join's backward, and rows of more than 2 pieces a thread, 512 with 128 (the join's spills at 112).
+constexpr int NORM_FWD_THREADS = 768;
+constexpr int norm_bwd_threads(bool join, int nv) { return join || nv > 2 ? 512 : 576; }
 
 // Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.
 template <class T, int NV, bool RING, bool JOIN>
@@ -157,7 +155,7 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
   const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
   RowSum row_sum{red, tpr, row, 0};
-  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, sh.stages, 0};
+  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, 0};
   const float inv_d = 1.f / (float)p.d;
   const int step = gridDim.x * sh.rpb;
   const size_t stride = (size_t)step * np;
@@ -179,9 +177,8 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   };
   row_sum.init();
   long long tile = (long long)blockIdx.x * sh.rpb;
-  size_t at = (size_t)(tile + row) * np + tg, ahead = at;
-  if (RING)
-    for (int i = 0; i < sh.stages - 1; ++i, ahead += stride) fetch(i, tile + (long long)i * step, ahead);
+  size_t at = (size_t)(tile + row) * np + tg;
+  if (RING) fetch(0, tile, at);
   float2 wp[JOIN ? NV : 1][H], wn[NV][H];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -191,12 +188,11 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   }
   const bool gated = JOIN && p.gate != nullptr;
   float gate = gated && tile + row < p.T ? p.gate[tile + row] : 1.f;
-  for (; tile < p.T; tile += step, at += stride, ring.next()) {
+  for (; tile < p.T; tile += step, at += stride, ring.stage ^= 1) {
     const long long t = tile + row;
     const bool live = t < p.T;
     if (RING) {
-      fetch(ring.oldest(), tile + (long long)(sh.stages - 1) * step, ahead);
-      ahead += stride;
+      fetch(ring.stage ^ 1, tile + step, at + stride);
       ring.wait();
     }
     float2 x[NV][H];
@@ -252,7 +248,7 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
 //   s1 = <w_next dN, x>,  G = dXo + r_o w_next dN - (r_o^2 (r_o s1 / d)) x,   s2 = <w_post G, y>,  dgate = b r_y s2,
 //   dY = (b gate r_y) w_post G - (b gate r_y (r_y (r_y s2 / d))) y
 template <class T, int NV, bool RING, bool JOIN>
-__global__ void __launch_bounds__(NORM_BWD_THREADS)
+__global__ void __launch_bounds__(JOIN || NV > 2 ? 512 : 576)
 norm_bwd_kernel(const NormArgs p, const RowShape sh) {
   constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 4 : 3;
   enum { DN, XO, DXO, YY };
@@ -261,7 +257,7 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
   __shared__ __align__(16) float red[2][NORM_WIDE_ROWS][NORM_MAX_WARPS];
   const int tpr = sh.tpr, row = threadIdx.x / tpr, tg = threadIdx.x - row * tpr, np = p.d / P;
   RowSum row_sum{red, tpr, row, 0};
-  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, sh.stages, 0};
+  RowRing<NT, NV, RING> ring{smem_u32(ring_smem) + threadIdx.x * 16, blockDim.x * 16, 0};
   const float inv_d = 1.f / (float)p.d;
   const int step = gridDim.x * sh.rpb;
   const size_t stride = (size_t)step * np;
@@ -287,9 +283,8 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
   };
   row_sum.init();
   long long tile = (long long)blockIdx.x * sh.rpb;
-  size_t at = (size_t)(tile + row) * np + tg, ahead = at;
-  if (RING)
-    for (int i = 0; i < sh.stages - 1; ++i, ahead += stride) fetch(i, tile + (long long)i * step, ahead);
+  size_t at = (size_t)(tile + row) * np + tg;
+  if (RING) fetch(0, tile, at);
   float2 wp[JOIN ? NV : 1][H], wn[NV][H], acc_p[JOIN ? NV : 1][H], acc_n[NV][H];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -311,14 +306,13 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
     if (JOIN && p.gate) gate = p.gate[t];
   };
   scalars(tile + row);
-  for (; tile < p.T; tile += step, at += stride, ring.next()) {
+  for (; tile < p.T; tile += step, at += stride, ring.stage ^= 1) {
     const long long t = tile + row;
     const bool live = t < p.T;
     const float ro = r_o, ry = r_y, ga = gate;
     scalars(t + step);
     if (RING) {
-      fetch(ring.oldest(), tile + (long long)(sh.stages - 1) * step, ahead);
-      ahead += stride;
+      fetch(ring.stage ^ 1, tile + step, at + stride);
       ring.wait();
     }
     float2 G[NV][H];
@@ -461,41 +455,35 @@ static etr_status norm_ptrs(std::initializer_list<const void*> need, std::initia
   return ETR_OK;
 }
 
-// Rows on threads.  2 pieces a thread, 4 or 8 where 512 threads would not hold the row; about 256 threads a block.
+// Rows on threads.  2 pieces a thread, 4 or 8 where 512 threads would not hold the row; about 256 threads a block, or 128 where
+// more threads fit an SM of `threads` then (three warps a row, join backward of 20000 x 1088: 71 and 75 % of the copy rate).
 static int norm_pieces(int d, int dtype) { return d * (int)elem_bytes(dtype) / 16; }
 static int norm_nv(int pieces) { return pieces <= 1024 ? 2 : pieces <= 2048 ? 4 : 8; }
-static RowShape norm_shape(int pieces) {
+static RowShape norm_shape(int pieces, int threads) {
   const int nv = norm_nv(pieces);
-  RowShape s = {4, 1, 0};
+  RowShape s = {4, 1};
   if (pieces <= 64)
     while (2 * s.tpr < pieces) s.tpr *= 2;
   else
     s.tpr = ceil_div(pieces, 32 * nv) * 32;
-  s.rpb = s.tpr < 256 ? 256 / s.tpr : 1;
+  const int wide = s.tpr < 256 ? 256 / s.tpr : 1, narrow = s.tpr < 128 ? 128 / s.tpr : 1;
+  s.rpb = threads / (s.tpr * wide) * wide >= threads / (s.tpr * narrow) * narrow ? wide : narrow;
   return s;
 }
 
 template <template <class, int> class K, class T>
 static etr_status norm_by_shape(const NormArgs& p, cudaStream_t st) {
-  const int pieces = p.d / PIECE<T>;
-  const RowShape s = norm_shape(pieces);
-  switch (norm_nv(pieces)) {
-    case 2: return K<T, 2>::run(p, s, st);
-    case 4: return K<T, 4>::run(p, s, st);
-  }
-  return K<T, sizeof(T) == 2 ? 4 : 8>::run(p, s, st);      // 8: fp32 rows only
+  const int nv = norm_nv(p.d / PIECE<T>);
+  return nv == 2 ? K<T, 2>::run(p, st) : nv == 4 ? K<T, 4>::run(p, st) : K<T, sizeof(T) == 2 ? 4 : 8>::run(p, st);      // 8: fp32 rows only
 }
 template <template <class, int> class K>
 static etr_status norm_by_type(int dtype, const NormArgs& p, cudaStream_t st) {
   return dtype == ETR_BF16 ? norm_by_shape<K, __nv_bfloat16>(p, st) : norm_by_shape<K, float>(p, st);
 }
 
-// A ring of three tiles, or two, within the CTA's part of 200 KiB; 0: rows so long that two tiles do not fit are read without
-// a ring.
-static int ring_stages(long long tile, int ctas) {
-  const long long n = 200 * 1024 / ctas / tile;
-  return n < 2 ? 0 : n < 3 ? 2 : 3;
-}
+static int norm_ctas(const RowShape& s, int threads) { return threads / (s.tpr * s.rpb) > 1 ? threads / (s.tpr * s.rpb) : 1; }
+// Whether two tiles fit the CTA's part of 200 KiB.
+static bool norm_ring(size_t tile, int ctas) { return 2 * tile * ctas <= 200 * 1024; }
 
 template <class K>
 static etr_status norm_launch(const char* name, K kernel, std::atomic<unsigned long long>& done, size_t smem, int ctas, const NormArgs& p,
@@ -511,52 +499,49 @@ static etr_status norm_launch(const char* name, K kernel, std::atomic<unsigned l
 template <class T, int NV>
 struct FwdRun {
   template <bool JOIN>
-  static etr_status go(const char* name, const NormArgs& p, RowShape s, cudaStream_t st) {
+  static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
     static std::atomic<unsigned long long> done{0}, done0{0};
-    const int block = s.tpr * s.rpb, threads = NV > 2 ? 512 : NORM_FWD_THREADS, ctas = threads / block > 1 ? threads / block : 1;
-    const long long tile = (JOIN ? 2ll : 1ll) * NV * block * 16;
-    s.stages = ring_stages(tile, ctas);
-    if (NV > 2 && s.stages == 0) return norm_launch(name, norm_fwd_kernel<T, NV, NV <= 2, JOIN>, done0, 0, ctas, p, s, st);
-    return norm_launch(name, norm_fwd_kernel<T, NV, true, JOIN>, done, (size_t)(s.stages * tile), ctas, p, s, st);
+    const int threads = NV > 2 ? 512 : NORM_FWD_THREADS;
+    const RowShape s = norm_shape(p.d / PIECE<T>, threads);
+    const int ctas = norm_ctas(s, threads);
+    const size_t tile = (size_t)(JOIN ? 2 : 1) * NV * s.tpr * s.rpb * 16;
+    if (NV > 2 && !norm_ring(tile, ctas)) return norm_launch(name, norm_fwd_kernel<T, NV, NV <= 2, JOIN>, done0, 0, ctas, p, s, st);
+    return norm_launch(name, norm_fwd_kernel<T, NV, true, JOIN>, done, 2 * tile, ctas, p, s, st);
   }
-  static etr_status run(const NormArgs& p, const RowShape& s, cudaStream_t st) {
-    return p.Y ? go<true>("join_kernel", p, s, st) : go<false>("prenorm_kernel", p, s, st);
-  }
+  static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_kernel", p, st) : go<false>("prenorm_kernel", p, st); }
 };
 
-static int norm_bwd_ctas(const RowShape& s) { return NORM_BWD_THREADS / (s.tpr * s.rpb) > 1 ? NORM_BWD_THREADS / (s.tpr * s.rpb) : 1; }
 // Blocks of the backward kernels, each of which leaves a row of partial sums per gain; at most NORM_BWD_MOST an SM.
-constexpr int NORM_BWD_MOST = 3;                  // blocks of 160 threads
-static int norm_bwd_blocks(int T, int d, int dtype) {
-  const RowShape s = norm_shape(norm_pieces(d, dtype));
-  const long long want = ((long long)T + s.rpb - 1) / s.rpb, most = (long long)current_sm_count() * norm_bwd_ctas(s);
+constexpr int NORM_BWD_MOST = 5;                  // blocks of 96 threads
+static int norm_bwd_blocks(int T, int d, int dtype, bool join) {
+  const int pieces = norm_pieces(d, dtype), threads = norm_bwd_threads(join, norm_nv(pieces));
+  const RowShape s = norm_shape(pieces, threads);
+  const long long want = ((long long)T + s.rpb - 1) / s.rpb, most = (long long)current_sm_count() * norm_ctas(s, threads);
   return (int)(want < most ? want : most);
 }
 
 template <class T, int NV>
 struct BwdRun {
   template <bool JOIN>
-  static etr_status go(const char* name, const NormArgs& p, RowShape s, cudaStream_t st) {
+  static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
     static std::atomic<unsigned long long> done{0}, done0{0};
-    const int block = s.tpr * s.rpb, ctas = norm_bwd_ctas(s);
-    const long long tile = (JOIN ? 4ll : 3ll) * NV * block * 16, fold = s.rpb > 1 ? (long long)s.rpb * p.d * 4 : 0;
-    s.stages = ring_stages(tile, ctas);
-    if (NV > 2 && s.stages == 0) return norm_launch(name, norm_bwd_kernel<T, NV, NV <= 2, JOIN>, done0, (size_t)fold, ctas, p, s, st);
-    const long long smem = s.stages * tile;
-    return norm_launch(name, norm_bwd_kernel<T, NV, true, JOIN>, done, (size_t)(smem > fold ? smem : fold), ctas, p, s, st);
+    constexpr int threads = norm_bwd_threads(JOIN, NV);
+    const RowShape s = norm_shape(p.d / PIECE<T>, threads);
+    const int ctas = norm_ctas(s, threads);
+    const size_t tile = (size_t)(JOIN ? 4 : 3) * NV * s.tpr * s.rpb * 16, fold = s.rpb > 1 ? (size_t)s.rpb * p.d * 4 : 0;
+    if (NV > 2 && !norm_ring(tile, ctas)) return norm_launch(name, norm_bwd_kernel<T, NV, NV <= 2, JOIN>, done0, fold, ctas, p, s, st);
+    return norm_launch(name, norm_bwd_kernel<T, NV, true, JOIN>, done, 2 * tile > fold ? 2 * tile : fold, ctas, p, s, st);
   }
-  static etr_status run(const NormArgs& p, const RowShape& s, cudaStream_t st) {
-    return p.Y ? go<true>("join_bwd_kernel", p, s, st) : go<false>("prenorm_bwd_kernel", p, s, st);
-  }
+  static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_bwd_kernel", p, st) : go<false>("prenorm_bwd_kernel", p, st); }
 };
 
-static etr_status norm_dw(const etr_norm_config* c, const NormArgs& p, float* dw_next, float* dw_post, cudaStream_t st) {
+static etr_status norm_dw(const etr_norm_config* c, bool join, const NormArgs& p, float* dw_next, float* dw_post, cudaStream_t st) {
   if (dw_next == nullptr && dw_post == nullptr) return ETR_OK;
   const bool both = dw_next && dw_post;
   const float* a = dw_next ? p.part_next : p.part_post;
   ETR_TIME_BEGIN("norm_dw_kernel");
   launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 1024, 0, st, 1, a, (const float*)p.part_post, dw_next ? dw_next : dw_post,
-                dw_post, norm_bwd_blocks(c->T, c->d, c->dtype), c->d);
+                dw_post, norm_bwd_blocks(c->T, c->d, c->dtype, join), c->d);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
 }
@@ -613,7 +598,7 @@ etr_status etr_prenorm_bwd(const etr_norm_config* c, const void* dN, const void*
   p.dN = dN; p.Xo_in = X; p.w_next = w; p.rstd_o = rstd; p.dXo = dres; p.dX = dX;
   p.part_next = dw ? (float*)ws : nullptr;
   if (c->T > 0) ETR_TRY(norm_by_type<BwdRun>(c->dtype, p, (cudaStream_t)stream));
-  return norm_dw(c, p, dw, nullptr, (cudaStream_t)stream);
+  return norm_dw(c, false, p, dw, nullptr, (cudaStream_t)stream);
 }
 
 etr_status etr_join_bwd(const etr_norm_config* c, const void* dXo, const void* dN, const void* Y, const void* Xo, const float* w_post,
@@ -635,7 +620,7 @@ etr_status etr_join_bwd(const etr_norm_config* c, const void* dXo, const void* d
   p.part_next = dw_next ? (float*)ws : nullptr;
   p.part_post = dw_post ? (float*)ws + (size_t)current_sm_count() * NORM_BWD_MOST * c->d : nullptr;
   if (c->T > 0) ETR_TRY(norm_by_type<BwdRun>(c->dtype, p, (cudaStream_t)stream));
-  return norm_dw(c, p, dw_next, dw_post, (cudaStream_t)stream);
+  return norm_dw(c, true, p, dw_next, dw_post, (cudaStream_t)stream);
 }
 
 }  // extern "C"
