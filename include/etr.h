@@ -458,7 +458,7 @@ etr_status etr_sort_validate(const etr_sort_config* cfg);
 int64_t etr_sort_n_rows(const etr_sort_config* cfg);
 /* Size of a block for the plan (need, may be NULL) and its carving (out, may be NULL; base 256-byte aligned). */
 etr_status etr_sort_plan_bind(const etr_sort_config* cfg, void* base, size_t bytes, etr_sort_plan* out, size_t* need);
-/* topk_idx [T,k] int32.  Fills every member of the plan.  One launch, two where T*k > 32768. */
+/* topk_idx [T,k] int32.  Fills every member of the plan.  One launch, two where T*k > 65536. */
 etr_status etr_sort(const etr_sort_config* cfg, const int32_t* topk_idx, const etr_sort_plan* plan, void* stream);
 /* Xs[pos[t][j],:] = X[t,:]; pad rows 0. */
 etr_status etr_sort_rows(const etr_sort_config* cfg, const void* X, const etr_sort_plan* plan, void* Xs, void* stream);

@@ -139,15 +139,16 @@ struct RowRing {
   }
 };
 
-// Threads of an SM, which is what the launch bounds ask for (a block has at most 512): forward 768 with at most 80 registers each;
-// prenorm's backward 576 with 112, which fits a third block of 192 threads (20000 x 1088: 49 % of the copy rate with two, 76
-// with three); the join's backward, and rows of more than 2 pieces a thread, 512 with 128 (the join's spills at 112).
-constexpr int NORM_FWD_THREADS = 768;
+// Threads of an SM, which is what the launch bounds ask for (a block has at most 512): forward 768 with at most 80 registers each,
+// and 1024 with 64 for a prenorm whose block is more than 384 threads, so that two fit (fp32 40920 x 3280: 72 % of the copy
+// rate with one, 97 with two; smaller blocks lose: 20000 x 1088 bf16 75 and 67 %); prenorm's backward 576 with 112, which fits a
+// third block of 192 threads (20000 x 1088: 49 % with two, 76 with three); the join's backward, and rows of more than 2
+// pieces a thread, 512 with 128 (the join's spills at 112).
 constexpr int norm_bwd_threads(bool join, int nv) { return join || nv > 2 ? 512 : 576; }
 
 // Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.
-template <class T, int NV, bool RING, bool JOIN>
-__global__ void __launch_bounds__(NV > 2 ? 512 : NORM_FWD_THREADS)
+template <class T, int NV, bool RING, bool JOIN, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   constexpr int P = PIECE<T>, H = P / 2, NT = JOIN ? 2 : 1, XX = 0, YY = NT - 1;
   grid_sync();
@@ -415,7 +416,7 @@ norm_bwd_kernel(const NormArgs p, const RowShape sh) {
 }
 
 // dw[c] = sum over the blocks' partial rows, in a fixed order; grid y: which weight.  32 columns a block, every warp a 32nd of the
-// rows (some ten of them, their loads in flight together).
+// rows (some ten of them, their loads in flight together; fewer warps took longer even for few rows).
 __global__ void __launch_bounds__(1024)
 norm_dw_kernel(const float* part0, const float* part1, float* __restrict__ dw0, float* __restrict__ dw1, int rows, int d) {
   grid_sync();
@@ -485,6 +486,10 @@ static int norm_ctas(const RowShape& s, int threads) { return threads / (s.tpr *
 // Whether two tiles fit the CTA's part of 200 KiB.
 static bool norm_ring(size_t tile, int ctas) { return 2 * tile * ctas <= 200 * 1024; }
 
+// Rows of 2 pieces a thread always have a ring; those of more are one to a block of 288 to 512 threads.
+constexpr bool always_ring(int slots, int nv) { return nv <= 2 || 2 * slots * 512 * 16 <= 200 * 1024; }
+constexpr bool sometimes_ring(int slots, int nv) { return nv <= 2 || 2 * slots * 288 * 16 <= 200 * 1024; }
+
 template <class K>
 static etr_status norm_launch(const char* name, K kernel, std::atomic<unsigned long long>& done, size_t smem, int ctas, const NormArgs& p,
                               const RowShape& s, cudaStream_t st) {
@@ -500,13 +505,22 @@ template <class T, int NV>
 struct FwdRun {
   template <bool JOIN>
   static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
-    static std::atomic<unsigned long long> done{0}, done0{0};
-    const int threads = NV > 2 ? 512 : NORM_FWD_THREADS;
-    const RowShape s = norm_shape(p.d / PIECE<T>, threads);
-    const int ctas = norm_ctas(s, threads);
-    const size_t tile = (size_t)(JOIN ? 2 : 1) * NV * s.tpr * s.rpb * 16;
-    if (NV > 2 && !norm_ring(tile, ctas)) return norm_launch(name, norm_fwd_kernel<T, NV, NV <= 2, JOIN>, done0, 0, ctas, p, s, st);
-    return norm_launch(name, norm_fwd_kernel<T, NV, true, JOIN>, done, 2 * tile, ctas, p, s, st);
+    if constexpr (NV == 2 && !JOIN)
+      if (p.d / PIECE<T> > 768) return with<JOIN, 1024>(name, p, st);
+    return with<JOIN, (NV > 2 ? 512 : 768)>(name, p, st);
+  }
+  template <bool JOIN, int THREADS>
+  static etr_status with(const char* name, const NormArgs& p, cudaStream_t st) {
+    const RowShape s = norm_shape(p.d / PIECE<T>, THREADS);
+    const int ctas = norm_ctas(s, THREADS);
+    constexpr int slots = (JOIN ? 2 : 1) * NV;
+    const size_t tile = (size_t)slots * s.tpr * s.rpb * 16;
+    if constexpr (!always_ring(slots, NV)) {
+      static std::atomic<unsigned long long> done{0};
+      if (!norm_ring(tile, ctas)) return norm_launch(name, norm_fwd_kernel<T, NV, false, JOIN, THREADS>, done, 0, ctas, p, s, st);
+    }
+    static std::atomic<unsigned long long> done{0};
+    return norm_launch(name, norm_fwd_kernel<T, NV, true, JOIN, THREADS>, done, 2 * tile, ctas, p, s, st);
   }
   static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_kernel", p, st) : go<false>("prenorm_kernel", p, st); }
 };
@@ -524,13 +538,19 @@ template <class T, int NV>
 struct BwdRun {
   template <bool JOIN>
   static etr_status go(const char* name, const NormArgs& p, cudaStream_t st) {
-    static std::atomic<unsigned long long> done{0}, done0{0};
-    constexpr int threads = norm_bwd_threads(JOIN, NV);
+    constexpr int threads = norm_bwd_threads(JOIN, NV), slots = (JOIN ? 4 : 3) * NV;
     const RowShape s = norm_shape(p.d / PIECE<T>, threads);
     const int ctas = norm_ctas(s, threads);
-    const size_t tile = (size_t)(JOIN ? 4 : 3) * NV * s.tpr * s.rpb * 16, fold = s.rpb > 1 ? (size_t)s.rpb * p.d * 4 : 0;
-    if (NV > 2 && !norm_ring(tile, ctas)) return norm_launch(name, norm_bwd_kernel<T, NV, NV <= 2, JOIN>, done0, fold, ctas, p, s, st);
-    return norm_launch(name, norm_bwd_kernel<T, NV, true, JOIN>, done, 2 * tile > fold ? 2 * tile : fold, ctas, p, s, st);
+    const size_t tile = (size_t)slots * s.tpr * s.rpb * 16, fold = s.rpb > 1 ? (size_t)s.rpb * p.d * 4 : 0;
+    if constexpr (!always_ring(slots, NV)) {
+      static std::atomic<unsigned long long> done{0};
+      if (!norm_ring(tile, ctas)) return norm_launch(name, norm_bwd_kernel<T, NV, false, JOIN>, done, fold, ctas, p, s, st);
+    }
+    if constexpr (sometimes_ring(slots, NV)) {
+      static std::atomic<unsigned long long> done{0};
+      return norm_launch(name, norm_bwd_kernel<T, NV, true, JOIN>, done, 2 * tile > fold ? 2 * tile : fold, ctas, p, s, st);
+    }
+    return ETR_ERR_UNSUPPORTED;                  // not reached: a row of these sizes has a ring or has not
   }
   static etr_status run(const NormArgs& p, cudaStream_t st) { return p.Y ? go<true>("join_bwd_kernel", p, st) : go<false>("prenorm_bwd_kernel", p, st); }
 };
@@ -540,8 +560,8 @@ static etr_status norm_dw(const etr_norm_config* c, bool join, const NormArgs& p
   const bool both = dw_next && dw_post;
   const float* a = dw_next ? p.part_next : p.part_post;
   ETR_TIME_BEGIN("norm_dw_kernel");
-  launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 1024, 0, st, 1, a, (const float*)p.part_post, dw_next ? dw_next : dw_post,
-                dw_post, norm_bwd_blocks(c->T, c->d, c->dtype, join), c->d);
+  launch_kernel(norm_dw_kernel, dim3(ceil_div(c->d, 32), both ? 2 : 1), 1024, 0, st, 1, a, (const float*)p.part_post,
+                dw_next ? dw_next : dw_post, dw_post, norm_bwd_blocks(c->T, c->d, c->dtype, join), c->d);
   ETR_LAUNCH_CHECK();
   return ETR_OK;
 }

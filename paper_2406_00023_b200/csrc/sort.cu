@@ -14,7 +14,7 @@ constexpr int SORT_WARPS = 16;                   // at most
 constexpr int SORT_CLUSTER = 8;                   // CTAs of a cluster, where there are several
 constexpr int SORT_ALONE = 16;                    // CTAs at most of one that works alone
 constexpr int SORT_MAX_CLUSTERS = 18;            // 144 of the 148 SMs
-constexpr int SORT_ONE_CLUSTER = 32768;          // pairs that one cluster takes without a counting launch before it
+constexpr int SORT_ONE_CLUSTER = 65536;          // pairs that one cluster takes without a counting launch before it
 constexpr int SORT_RUN = 32;                     // pairs per warp that are worth another CTA
 
 struct SortShape {
@@ -192,17 +192,18 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   }
   // Rows without a token, an expert's at a time by one warp, or by several where there are more warps than experts; without
   // gaps between experts only those behind the last.
-  const bool gaps = s.align > 1;
-  const int first = gaps ? 0 : s.E - 1, spans = s.E - first, all_warps = gridDim.x * warps, parts = max(1, all_warps / spans);
-  for (int x = blockIdx.x * warps + warp; x < spans * parts; x += all_warps) {
-    const int e = first + x % spans, part = x / spans;
+  const int first = s.align > 1 ? 0 : s.E - 1, spans = s.E - first, all_warps = gridDim.x * warps, gw = blockIdx.x * warps + warp;
+  const int parts = max(1, all_warps / spans), share = gw / spans;           // parts > 1: one span a warp
+#pragma unroll 4
+  for (int x = parts > 1 ? gw - share * spans : gw; x < spans && (parts == 1 || share < parts); x += all_warps) {
+    const int e = first + x;
     const int lo = start[e] + used[e], hi = e + 1 < s.E ? start[e + 1] : s.n_rows;
     const int lo4 = min((lo + 3) & ~3, hi), hi4 = max(hi & ~3, lo4);
-    if (part == 0) {
+    if (parts == 1 || share == 0) {
       if (lo + lane < lo4) row_token[lo + lane] = -1;
       if (hi4 + lane < hi) row_token[hi4 + lane] = -1;
     }
-    for (int r = lo4 + 4 * (lane + 32 * part); r < hi4; r += 128 * parts) *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
+    for (int r = lo4 + 4 * (lane + 32 * (parts > 1 ? share : 0)); r < hi4; r += 128 * parts) *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
   }
   if (blockIdx.x == 0 && tid == 0) {
     int end = 0, all = 0, with = 0;
@@ -213,15 +214,15 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   if (ncta > 1) cluster.barrier_wait();          // no CTA leaves while another may still read its counts
 }
 
-// Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first PAD_SHARES * E blocks of a
-// row pass write them, so that they do not end up as its tail.
-constexpr int PAD_SHARES = 8;
+// Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first blocks of a row pass, one
+// an expert for every 16 rows of `align` up to 8, write them, so that they do not end up as its tail.
+__host__ __device__ constexpr int pad_shares(int align) { return align >= 128 ? 8 : (align + 15) / 16; }
 __device__ __forceinline__ void zero_pad_rows(uint4* rows, int nv, const int32_t* counts, const int32_t* offsets, int align) {
-  const int e = blockIdx.x / PAD_SHARES, share = blockIdx.x % PAD_SHARES;
+  const int shares = pad_shares(align), e = blockIdx.x / shares, share = blockIdx.x % shares;
   const int c = counts[e], pads = (c + align - 1) / align * align - c;
   uint4* dst = rows + ((size_t)offsets[e] + c) * nv;
   const size_t n = (size_t)pads * nv;
-  for (size_t v = share * 256 + threadIdx.x; v < n; v += PAD_SHARES * 256) dst[v] = make_uint4(0, 0, 0, 0);
+  for (size_t v = share * 256 + threadIdx.x; v < n; v += shares * 256) dst[v] = make_uint4(0, 0, 0, 0);
 }
 
 // Xs[pos[t][j]] = X[t].  Token-major, so that a token is read once however many experts it has.  X is a flat run of
@@ -257,7 +258,8 @@ sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, cons
 
 // Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.  A
 // thread has one 16-byte piece of a token and asks for AHEAD rows' pieces before it adds them: 2 at full occupancy for k <= 2, else 4
-// at three quarters of it (65536 x 4096 bf16, k = 2: 302 and 322 us; 6113 x 2048, k = 8: 41 and 36.5).
+// at three quarters of it (65536 x 4096 bf16, k = 2: 302 and 322 us; 6113 x 2048, k = 8: 41 and 36.5).  (unsort_one_kernel: k = 1 and
+// many pieces.)
 template <class T, int AHEAD>
 __global__ void __launch_bounds__(256, AHEAD > 2 ? 6 : 8)
 unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv, int k) {
@@ -294,12 +296,45 @@ unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __re
   Y[base + (int)threadIdx.x] = pack<T>(acc);
 }
 
+// unsort_kernel for k = 1 where the SMs have pieces enough: UNSORT_PIECES a thread in flight (28577 x 1632 bf16: 68 % of the
+// copy rate with one, 95 with four; 100 x 1632: 1.6 and 2.1 us).
+constexpr int UNSORT_PIECES = 4;
+template <class T>
+__global__ void __launch_bounds__(256)
+unsort_one_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv) {
+  constexpr int P = PIECE<T>;
+  grid_sync();
+  const long long base = (long long)blockIdx.x * (256 * UNSORT_PIECES);
+  const long long t0 = base / nv;
+  const int r0 = (int)(base - t0 * nv);
+  uint4 q[UNSORT_PIECES];
+  float f[UNSORT_PIECES];
+#pragma unroll
+  for (int u = 0; u < UNSORT_PIECES; ++u) {
+    const int i = u * 256 + (int)threadIdx.x;
+    const unsigned dt = (unsigned)(r0 + i) / (unsigned)nv;
+    const int r = base + i < n ? pos[t0 + dt] : -1;
+    q[u] = r >= 0 ? rows[(size_t)r * nv + (r0 + i - (int)dt * nv)] : make_uint4(0, 0, 0, 0);
+    f[u] = r >= 0 && w ? w[t0 + dt] : 1.f;
+  }
+#pragma unroll
+  for (int u = 0; u < UNSORT_PIECES; ++u) {
+    const long long i = base + u * 256 + threadIdx.x;
+    if (i >= n) break;
+    float x[P];
+    unpack<T>(q[u], x);
+#pragma unroll
+    for (int e = 0; e < P; ++e) x[e] *= f[u];
+    Y[i] = pack<T>(x);
+  }
+}
+
 // dO[pos[t][j]] = w[t][j] dY[t], dw[t][j] = <dY[t], O[pos[t][j]]>; L lanes per pair (a warp, or the power of two that holds a
 // short row).  The pairs of a token are neighbours, so its dY comes from HBM once.
 template <class T>
 __global__ void __launch_bounds__(256)
 unsort_bwd_kernel(const uint4* dY, const uint4* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
-                  uint4* __restrict__ dO, float* __restrict__ dw, long long pairs, int k, int nv, int L, int align, int pad_blocks) {
+                  uint4* __restrict__ dO, float* __restrict__ dw, int pairs, int k, int nv, int L, int align, int pad_blocks) {
   constexpr int P = PIECE<T>, AHEAD = 4;
   grid_sync();
   if ((int)blockIdx.x < pad_blocks) return zero_pad_rows(dO, nv, counts, offsets, align);
@@ -334,6 +369,72 @@ unsort_bwd_kernel(const uint4* dY, const uint4* O, const float* w, const int32_t
   }
   for (int s = L >> 1; s > 0; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
   if (lane == 0 && i < pairs) dw[i] = dot;
+}
+
+// The same for rows of at most 32 SHORT_STEPS pieces.  Such a pair is over so soon that a warp spends its time waiting for the
+// pair's row number, then for the row; here blocks walk pairs in strides, the next pair's pieces are copied ahead into the
+// lane's own slots of shared memory (cp.async) and the row of the one after it asked for.  7738 x 752 bf16, k = 4: 24.3 us
+// as above, 19.2 so; but 16384 x 2048, k = 2: 51.7 as above, 55.8 with such a ring.
+constexpr int SHORT_STEPS = 4, SHORT_SMEM = 2 * 2 * SHORT_STEPS * 256 * 16, SHORT_CTAS = 3;
+template <class T>
+__global__ void __launch_bounds__(256, SHORT_CTAS)
+unsort_bwd_short_kernel(const uint4* dY, const uint4* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
+                        uint4* __restrict__ dO, float* __restrict__ dw, int pairs, int k, int nv, int L, int align, int pad_blocks) {
+  constexpr int P = PIECE<T>, N = SHORT_STEPS;
+  grid_sync();
+  if ((int)blockIdx.x < pad_blocks) return zero_pad_rows(dO, nv, counts, offsets, align);
+  extern __shared__ uint4 slots[];
+  const uint32_t mine = smem_u32(slots) + threadIdx.x * 16;        // slot (stage, tensor, u): (stage * 2 N + tensor * N + u) * 4096 on
+  const int lane = threadIdx.x & (L - 1), per = 256 / L;
+  const long long stride = (long long)(gridDim.x - pad_blocks) * per;
+  long long i = (long long)(blockIdx.x - pad_blocks) * per + threadIdx.x / L;
+  int row = i < pairs ? pos[i] : -1, row2 = i + stride < pairs ? pos[i + stride] : -1;
+  float f = row >= 0 ? w[i] : 0.f;
+  auto fetch = [&](int stage, long long at, int r) {
+    if (r >= 0) {
+      const uint4* gy = dY + (size_t)((unsigned)at / (unsigned)k) * nv + lane;
+      const uint4* o = O + (size_t)r * nv + lane;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        if (lane + u * L >= nv) break;
+        const uint32_t dst = mine + (stage * 2 * N + u) * 4096;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(gy + u * L) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + N * 4096), "l"(o + u * L) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  fetch(0, i, row);
+  int stage = 0;
+  for (long long base = i - (threadIdx.x & 31) / L; base < pairs; base += stride, i += stride, stage ^= 1) {      // base: the warp's first pair
+    fetch(stage ^ 1, i + stride, row2);
+    const float f2 = row2 >= 0 ? w[i + stride] : 0.f;
+    const int row3 = i + 2 * stride < pairs ? pos[i + 2 * stride] : -1;
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    float dot = 0.f;
+    if (row >= 0) {
+      uint4* out = dO + (size_t)row * nv + lane;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        if (lane + u * L >= nv) break;
+        uint4 a, b;
+        const uint32_t src = mine + (stage * 2 * N + u) * 4096;
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w) : "r"(src) : "memory");
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(src + N * 4096) : "memory");
+        float x[P], y[P];
+        unpack<T>(a, x);
+        unpack<T>(b, y);
+#pragma unroll
+        for (int e = 0; e < P; ++e) { dot = fmaf(x[e], y[e], dot); x[e] *= f; }
+        out[u * L] = pack<T>(x);
+      }
+    }
+    for (int s = L >> 1; s > 0; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
+    if (lane == 0 && i < pairs) dw[i] = dot;
+    row = row2;
+    row2 = row3;
+    f = f2;
+  }
 }
 
 // ---- launches ----------------------------------------------------------------------------------
@@ -381,11 +482,12 @@ static bool ensure_wide_cluster(K kernel, std::atomic<unsigned long long>& done)
   return true;
 }
 
-static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? PAD_SHARES * c->E : 0; }
+static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? pad_shares(c->align) * c->E : 0; }
 
 // One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 16 of 16 warps (an opt-in size); longer batches take up to
 // 18 clusters of 8, and a launch before that counts the clusters' pairs.  Measured, a plan by itself: 32768 pairs of 32
-// experts 6.4 us in one cluster of 16, 8.4 of 8, 10 with the count; 131072 of 64 10.3 us with the count, 14.4 without.
+// experts 6.4 us in one cluster of 16, 8.4 of 8, 10 with the count; 65536 of 128 9.9 in one, 9.7 with the count; 131072 of 64
+// 14.4 and 10.3.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0}, wide{0};
   if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 4) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
@@ -424,7 +526,12 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   int L = 32;                                    // lanes per pair of unsort_bwd
   while (L > 1 && nv <= L / 2) L /= 2;
   const long long n = (long long)c->T * nv, pairs = (long long)c->T * c->k;
-  const long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + 256 - 1) / 256 : (pairs * L + 255) / 256;
+  const bool several = c->k == 1 && n > (long long)current_sm_count() * 2048 * 2;       // two rounds of every SM's threads
+  const int one = several ? 256 * UNSORT_PIECES : 256;
+  long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + one - 1) / one : (pairs * L + 255) / 256;
+  const long long walk = (long long)current_sm_count() * SHORT_CTAS;
+  const bool brief = which == 2 && nv <= 32 * SHORT_STEPS && blocks > walk;       // a walk of one pair gains nothing
+  if (brief) blocks = walk;
   if (blocks + pad >= (1ll << 31)) return ETR_ERR_SHAPE;
   switch (which) {
     case 0:
@@ -434,13 +541,20 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
       break;
     case 1:
       ETR_TIME_BEGIN("unsort_kernel");
-      launch_kernel(c->k > 2 ? unsort_kernel<T, 4> : unsort_kernel<T, 2>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
+      if (several)
+        launch_kernel(unsort_one_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv);
+      else
+        launch_kernel(c->k > 2 ? unsort_kernel<T, 4> : unsort_kernel<T, 2>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n,
+                      nv, c->k);
       break;
-    case 2:
+    case 2: {
+      static std::atomic<unsigned long long> done{0};
+      if (brief && !ensure_dyn_smem(unsort_bwd_short_kernel<T>, SHORT_SMEM, done)) return ETR_ERR_CUDA;
       ETR_TIME_BEGIN("unsort_bwd_kernel");
-      launch_kernel(unsort_bwd_kernel<T>, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, (const uint4*)b, w, p->pos, p->counts,
-                    p->offsets, (uint4*)out, dw, pairs, c->k, nv, L, c->align, pad);
+      launch_kernel(brief ? unsort_bwd_short_kernel<T> : unsort_bwd_kernel<T>, (unsigned)(blocks + pad), 256, brief ? (size_t)SHORT_SMEM : 0, st, 1,
+                    (const uint4*)a, (const uint4*)b, w, p->pos, p->counts, p->offsets, (uint4*)out, dw, (int)pairs, c->k, nv, L, c->align, pad);
       break;
+    }
   }
   ETR_LAUNCH_CHECK();
   return ETR_OK;

@@ -13,7 +13,8 @@ DT = {torch.bfloat16: etr.BF16, torch.float32: etr.F32}
 TYPES = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 EPS, A, B = 1e-6, 0.875, 0.5
 SIZES = [(1, 8), (3, 64), (2, 256), (17, 264), (9, 512), (5, 520), (33, 768), (64, 1024), (31, 1088), (7, 2048), (300, 2056), (13, 4096),
-         (5, 8192), (3, 8200), (4, 16384), (2000, 16), (1531, 768)]
+         (5, 8192), (3, 8200), (4, 16384), (2000, 16), (1531, 768),
+         (2500, 1088), (1300, 4096), (700, 8192), (300, 12288)]
 
 
 def tensors(T, d, dtype, seed):
