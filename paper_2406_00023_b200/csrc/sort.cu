@@ -256,16 +256,16 @@ sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, cons
   }
 }
 
-// Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.  A
-// thread has one 16-byte piece of a token and asks for AHEAD rows' pieces before it adds them: 2 at full occupancy for k <= 2, else 4
-// at three quarters of it (65536 x 4096 bf16, k = 2: 302 and 322 us; 6113 x 2048, k = 8: 41 and 36.5).  (unsort_one_kernel: k = 1 and
-// many pieces.)
-template <class T, int AHEAD>
-__global__ void __launch_bounds__(256, AHEAD > 2 ? 6 : 8)
+// Y[t] = sum_j w[t][j] rows[pos[t][j]], pairs without a row left out (w == nullptr: plain sum).  Sums in fp32, j ascending.  HBM-bound:
+// what counts is loads in flight.  Any k: a 16-byte piece of a token a thread, four rows' pieces asked for before they are
+// added (10 blocks of 128 threads an SM: 6113 x 2048 bf16, k = 8 34.1 us; 256 threads at 8, 6 and 5 blocks 40.8, 36.5, 34.7).
+constexpr int UNSORT_THREADS = 128, UNSORT_AHEAD = 4;
+template <class T>
+__global__ void __launch_bounds__(UNSORT_THREADS, 10)
 unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv, int k) {
-  constexpr int P = PIECE<T>;
+  constexpr int P = PIECE<T>, AHEAD = UNSORT_AHEAD;
   grid_sync();
-  const long long base = (long long)blockIdx.x * 256;
+  const long long base = (long long)blockIdx.x * UNSORT_THREADS;
   const long long t0 = base / nv;
   const int i = (int)(base - t0 * nv) + (int)threadIdx.x;
   if (base + (int)threadIdx.x >= n) return;
@@ -296,36 +296,46 @@ unsort_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __re
   Y[base + (int)threadIdx.x] = pack<T>(acc);
 }
 
-// unsort_kernel for k = 1 where the SMs have pieces enough: UNSORT_PIECES a thread in flight (28577 x 1632 bf16: 68 % of the
-// copy rate with one, 95 with four; 100 x 1632: 1.6 and 2.1 us).
-constexpr int UNSORT_PIECES = 4;
-template <class T>
-__global__ void __launch_bounds__(256)
-unsort_one_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv) {
-  constexpr int P = PIECE<T>;
+// k <= 4 and pieces enough for every SM: U pieces of all K rows a thread, known to the compiler (16384 x 4096 bf16, k = 2 59.6 us
+// against 77 in the form above, 20000 x 2048, k = 3 49.7 and 59; 28577 x 1632, k = 1 29.7 and 42).
+__host__ __device__ constexpr int unsort_few_pieces(int k) { return k <= 2 ? 4 : k == 3 ? 2 : 1; }
+template <class T, int K>
+__global__ void __launch_bounds__(UNSORT_THREADS)
+unsort_few_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* __restrict__ Y, long long n, int nv) {
+  constexpr int P = PIECE<T>, U = unsort_few_pieces(K);
   grid_sync();
-  const long long base = (long long)blockIdx.x * (256 * UNSORT_PIECES);
+  const long long base = (long long)blockIdx.x * (UNSORT_THREADS * U);
   const long long t0 = base / nv;
   const int r0 = (int)(base - t0 * nv);
-  uint4 q[UNSORT_PIECES];
-  float f[UNSORT_PIECES];
+  uint4 q[U][K];
+  float f[U][K];
 #pragma unroll
-  for (int u = 0; u < UNSORT_PIECES; ++u) {
-    const int i = u * 256 + (int)threadIdx.x;
+  for (int u = 0; u < U; ++u) {
+    const int i = u * UNSORT_THREADS + (int)threadIdx.x;
     const unsigned dt = (unsigned)(r0 + i) / (unsigned)nv;
-    const int r = base + i < n ? pos[t0 + dt] : -1;
-    q[u] = r >= 0 ? rows[(size_t)r * nv + (r0 + i - (int)dt * nv)] : make_uint4(0, 0, 0, 0);
-    f[u] = r >= 0 && w ? w[t0 + dt] : 1.f;
+    const int v = r0 + i - (int)dt * nv;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      const int r = base + i < n ? pos[(t0 + dt) * K + j] : -1;
+      q[u][j] = r >= 0 ? rows[(size_t)r * nv + v] : make_uint4(0, 0, 0, 0);
+      f[u][j] = r >= 0 && w ? w[(t0 + dt) * K + j] : 1.f;
+    }
   }
 #pragma unroll
-  for (int u = 0; u < UNSORT_PIECES; ++u) {
-    const long long i = base + u * 256 + threadIdx.x;
+  for (int u = 0; u < U; ++u) {
+    const long long i = base + u * UNSORT_THREADS + threadIdx.x;
     if (i >= n) break;
-    float x[P];
-    unpack<T>(q[u], x);
+    float acc[P];
 #pragma unroll
-    for (int e = 0; e < P; ++e) x[e] *= f[u];
-    Y[i] = pack<T>(x);
+    for (int e = 0; e < P; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      float x[P];
+      unpack<T>(q[u][j], x);
+#pragma unroll
+      for (int e = 0; e < P; ++e) acc[e] = fmaf(f[u][j], x[e], acc[e]);
+    }
+    Y[i] = pack<T>(acc);
   }
 }
 
@@ -526,8 +536,8 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   int L = 32;                                    // lanes per pair of unsort_bwd
   while (L > 1 && nv <= L / 2) L /= 2;
   const long long n = (long long)c->T * nv, pairs = (long long)c->T * c->k;
-  const bool several = c->k == 1 && n > (long long)current_sm_count() * 2048 * 2;       // two rounds of every SM's threads
-  const int one = several ? 256 * UNSORT_PIECES : 256;
+  const bool few = c->k <= 4 && n > (long long)current_sm_count() * 2048 * 2;      // two rounds of every SM's threads
+  const int one = few ? UNSORT_THREADS * unsort_few_pieces(c->k) : UNSORT_THREADS;
   long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + one - 1) / one : (pairs * L + 255) / 256;
   const long long walk = (long long)current_sm_count() * SHORT_CTAS;
   const bool brief = which == 2 && nv <= 32 * SHORT_STEPS && blocks > walk;       // a walk of one pair gains nothing
@@ -541,11 +551,11 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
       break;
     case 1:
       ETR_TIME_BEGIN("unsort_kernel");
-      if (several)
-        launch_kernel(unsort_one_kernel<T>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv);
+      if (few)
+        launch_kernel(c->k == 1 ? unsort_few_kernel<T, 1> : c->k == 2 ? unsort_few_kernel<T, 2> : c->k == 3 ? unsort_few_kernel<T, 3> : unsort_few_kernel<T, 4>,
+                      (unsigned)blocks, UNSORT_THREADS, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv);
       else
-        launch_kernel(c->k > 2 ? unsort_kernel<T, 4> : unsort_kernel<T, 2>, (unsigned)blocks, 256, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n,
-                      nv, c->k);
+        launch_kernel(unsort_kernel<T>, (unsigned)blocks, UNSORT_THREADS, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
       break;
     case 2: {
       static std::atomic<unsigned long long> done{0};

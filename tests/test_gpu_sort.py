@@ -77,7 +77,8 @@ def test_plan_of_long_batches(T, k, E, skew):
 ROWS = [(0, 2, 3, 16), (1, 1, 1, 8), (1, 8, 16, 64), (7, 3, 5, 72), (64, 2, 16, 1024), (129, 8, 128, 264), (300, 32, 7, 8),
         (513, 2, 16, 4096), (100, 3, 12, 1088), (50, 4, 9, 8200),
         # more pairs than the walking blocks of the weights' gradient have warps, more pieces than one round of every SM's threads
-        (2000, 3, 16, 512), (20000, 4, 16, 64), (3000, 1, 5, 2048), (40000, 1, 700, 136)]
+        (2000, 3, 16, 512), (20000, 4, 16, 64), (3000, 1, 5, 2048), (40000, 1, 700, 136),
+        (3000, 2, 5, 2048), (3001, 3, 5, 2056), (5000, 4, 9, 1088)]
 
 
 @pytest.mark.parametrize("T, k, E, d", ROWS)
