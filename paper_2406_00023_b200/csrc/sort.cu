@@ -226,33 +226,40 @@ __device__ __forceinline__ void zero_pad_rows(uint4* rows, int nv, const int32_t
 }
 
 // Xs[pos[t][j]] = X[t].  Token-major, so that a token is read once however many experts it has.  X is a flat run of
-// 16-byte pieces; a block takes SORT_PIECES of them.
-constexpr int SORT_UNROLL = 4, SORT_PIECES = 256 * SORT_UNROLL;
+// 16-byte pieces; a thread takes U of them, and asks for the rows of AHEAD pairs of each (four, or k where
+// that is fewer) before it stores.
+constexpr int SORT_PIECES = 4;                   // U of batches that fill the SMs; 1 for shorter ones
+template <int U, int AHEAD>
 __global__ void __launch_bounds__(256)
 sort_rows_kernel(const uint4* X, const int32_t* pos, const int32_t* counts, const int32_t* offsets, uint4* __restrict__ Xs, long long n,
                  int nv, int k, int align, int pad_blocks) {
   grid_sync();
   if ((int)blockIdx.x < pad_blocks) return zero_pad_rows(Xs, nv, counts, offsets, align);
-  const long long base = (long long)(blockIdx.x - pad_blocks) * SORT_PIECES;
+  const long long base = (long long)(blockIdx.x - pad_blocks) * (256 * U);
   const long long t0 = base / nv;
   const int r0 = (int)(base - t0 * nv);
-  uint4 q[SORT_UNROLL];
+  const int32_t* p0 = pos + t0 * k;
+  uint4 q[U];
+  int v[U], first[U];                            // piece of the row, first pair from t0's on; -1: behind the end
 #pragma unroll
-  for (int u = 0; u < SORT_UNROLL; ++u) {
-    const long long i = base + u * 256 + threadIdx.x;
-    if (i < n) q[u] = X[i];
-  }
-#pragma unroll
-  for (int u = 0; u < SORT_UNROLL; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int i = u * 256 + (int)threadIdx.x;
-    if (base + i >= n) break;
     const unsigned dt = (unsigned)(r0 + i) / (unsigned)nv;
-    const int v = r0 + i - (int)dt * nv;
-    const int32_t* p = pos + (t0 + dt) * k;
-    for (int j = 0; j < k; ++j) {
-      const int row = p[j];
-      if (row >= 0) Xs[(size_t)row * nv + v] = q[u];
-    }
+    v[u] = r0 + i - (int)dt * nv;
+    first[u] = base + i < n ? (int)dt * k : -1;
+    if (first[u] >= 0) q[u] = X[base + i];
+  }
+  for (int j0 = 0; j0 < k; j0 += AHEAD) {
+    int r[U][AHEAD];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) r[u][j] = first[u] >= 0 && j0 + j < k ? p0[first[u] + j0 + j] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j)
+        if (r[u][j] >= 0) Xs[(size_t)r[u][j] * nv + v[u]] = q[u];
   }
 }
 
@@ -538,7 +545,9 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   const long long n = (long long)c->T * nv, pairs = (long long)c->T * c->k;
   const bool few = c->k <= 4 && n > (long long)current_sm_count() * 2048 * 2;      // two rounds of every SM's threads
   const int one = few ? UNSORT_THREADS * unsort_few_pieces(c->k) : UNSORT_THREADS;
-  long long blocks = which == 0 ? (n + SORT_PIECES - 1) / SORT_PIECES : which == 1 ? (n + one - 1) / one : (pairs * L + 255) / 256;
+  const bool full = n > (long long)current_sm_count() * 256 * SORT_PIECES;
+  const int per = full ? 256 * SORT_PIECES : 256;
+  long long blocks = which == 0 ? (n + per - 1) / per : which == 1 ? (n + one - 1) / one : (pairs * L + 255) / 256;
   const long long walk = (long long)current_sm_count() * SHORT_CTAS;
   const bool brief = which == 2 && nv <= 32 * SHORT_STEPS && blocks > walk;       // a walk of one pair gains nothing
   if (brief) blocks = walk;
@@ -546,7 +555,7 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   switch (which) {
     case 0:
       ETR_TIME_BEGIN("sort_rows_kernel");
-      launch_kernel(sort_rows_kernel, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, p->pos, p->counts, p->offsets, (uint4*)out, n,
+      launch_kernel(!full ? sort_rows_kernel<1, 4> : c->k == 1 ? sort_rows_kernel<SORT_PIECES, 1> : c->k == 2 ? sort_rows_kernel<SORT_PIECES, 2> : sort_rows_kernel<SORT_PIECES, 4>, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, p->pos, p->counts, p->offsets, (uint4*)out, n,
                     nv, c->k, c->align, pad);
       break;
     case 1:
