@@ -450,7 +450,7 @@ typedef struct etr_sort_plan {
   int32_t* totals;            /* [4]    pairs with a row, pairs dropped, pairs without an expert, 0 */
   int32_t* row_token;         /* [etr_sort_n_rows] token of each row, -1 where there is none */
   int32_t* pos;               /* [T,k]  row of each pair, -1 where there is none */
-  int32_t* scratch;           /* [18 E] of etr_sort's own */
+  int32_t* scratch;           /* [18 E] of etr_sort's own (a plan serves one etr_sort at a time, captured graphs too) */
 } etr_sort_plan;
 
 etr_status etr_sort_validate(const etr_sort_config* cfg);
@@ -502,7 +502,8 @@ typedef struct etr_norm_config {
 } etr_norm_config;
 
 etr_status etr_norm_validate(const etr_norm_config* cfg);
-/* Scratch of the two backward calls: partial sums of the gains' gradients (does not depend on T). */
+/* Scratch of the two backward calls: partial sums of the gains' gradients (does not depend on T).  Nothing is kept in it from
+ * call to call; calls that may run at the same time need one each, captured graphs too. */
 etr_status etr_norm_workspace_bytes(const etr_norm_config* cfg, size_t* bytes);
 
 /* N[t,:] = X[t,:] r(X[t]) w;  rstd[t] = r(X[t]) (NULL: not wanted). */
@@ -514,7 +515,7 @@ etr_status etr_prenorm_bwd(const etr_norm_config* cfg, const void* dN, const voi
 /* X residual, Y the block's output, gate [T]:
  *   Xo = a X + b gate w_post (Y r(Y), or Y without post_norm);  N = Xo r(Xo) w_next
  * N NULL: no next norm (w_next and rstd_o are not used).  N is the norm of the fp32 sum before it is rounded to Xo.
- * rstd_y = r(Y) and rstd_o = r(Xo) are what the backward pass reads (NULL: not wanted). */
+ * rstd_y = r(Y) (post_norm only) and rstd_o = r(Xo) are what the backward pass reads (NULL: not wanted). */
 etr_status etr_join(const etr_norm_config* cfg, const void* X, const void* Y, const float* w_post, const float* gate,
                     const float* w_next, void* Xo, void* N, float* rstd_y, float* rstd_o, void* stream);
 /* From dXo (the sum's gradient from later in the residual stream) and dN, either of which may be NULL, with Y and Xo as the forward

@@ -12,6 +12,14 @@
 namespace {
 
 enum Kind { ACT_TD, ACT_RD, F32_D, F32_T, F32_TK, I32_TK, PLAN, SCRATCH };     // R: rows of the sorted buffers
+// A plan and the configuration that its memory was carved for (d and dtype do not matter to it).
+struct PlanFor {
+  etr_sort_plan plan;
+  etr_sort_config made;
+  bool fits(const etr_sort_config& c) const {
+    return made.T == c.T && made.k == c.k && made.E == c.E && made.align == c.align && made.capacity == c.capacity;
+  }
+};
 struct Arg { const char* name; Kind kind; bool optional; };
 struct Op { const char* name; bool sort; int n; Arg arg[15]; };
 
@@ -61,7 +69,7 @@ etr_status call(void* fn, int n, const void* c, void* const* a, void* st) {
   return ETR_ERR_ARG;
 }
 
-// run(op, config address, device, arguments...): 0, or (status, what was wrong).  Plans are addresses of etr_sort_plan; `device` is
+// run(op, config address, device, arguments...): 0, or (status, what was wrong).  Plans are addresses of PlanFor; `device` is
 // the one that the plan's memory is on, -1 where there is no plan.  Nothing here allocates or waits.
 PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   try {
@@ -83,8 +91,10 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       PyObject* o = args[3 + j];
       const Arg& w = op.arg[j];
       if (w.kind == PLAN) {
-        a[j] = PyLong_AsVoidPtr(o);
+        auto* p = static_cast<PlanFor*>(PyLong_AsVoidPtr(o));
         if (PyErr_Occurred()) return nullptr;
+        if (p == nullptr || !p->fits(*s)) return refuse(ETR_ERR_WORKSPACE, op, w, "made for another configuration");
+        a[j] = &p->plan;
         continue;
       }
       if (o == Py_None) {

@@ -392,6 +392,11 @@ class SortPlan(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("counts", "offsets", "totals", "row_token", "pos", "scratch")]
 
 
+class SortPlanFor(C.Structure):
+    """A plan and the configuration that its memory was carved for."""
+    _fields_ = [("plan", SortPlan), ("made", SortConfig)]
+
+
 SORT_MAX_K, SORT_MAX_E, NORM_MAX_D = 32, 1024, 16384
 
 
@@ -413,10 +418,11 @@ class SortBuffers:
     def __init__(self, cfg: SortConfig, device="cuda"):
         n = C.c_size_t(0)
         _check(lib().etr_sort_plan_bind(C.byref(cfg), None, C.c_size_t(0), None, C.byref(n)), "etr_sort_plan_bind")
-        self.cfg, self.n_rows = cfg, sort_n_rows(cfg)
+        self.n_rows = sort_n_rows(cfg)
         self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         base = (self.block.data_ptr() + 255) // 256 * 256
-        self.c = SortPlan()
+        both = SortPlanFor(made=cfg)               # a copy of cfg
+        self.c, self.cfg = both.plan, both.made
         _check(lib().etr_sort_plan_bind(C.byref(cfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_sort_plan_bind")
         for name, shape in (("counts", (cfg.E,)), ("offsets", (cfg.E + 1,)), ("totals", (4,)), ("row_token", (self.n_rows,)),
                             ("pos", (cfg.T, cfg.k))):
@@ -424,7 +430,7 @@ class SortBuffers:
             for m in shape:
                 count *= m
             setattr(self, name, self.block[off:off + 4 * count].view(torch.int32).view(shape))
-        self.ptr = C.addressof(self.c)
+        self._both, self.ptr = both, C.addressof(both)
         self.device = self.block.get_device()          # -1: not on a GPU, which every call refuses
 
 
@@ -519,12 +525,19 @@ def routed_sort_config(cfg: Config) -> SortConfig:
     return make_sort_config(T=cfg.T, k=cfg.k, E=cfg.E, d=cfg.d, dtype=cfg.dtype, align=128, capacity=cfg.capacity)
 
 
+def _routed_plan(where, cfg, plan):
+    if bytes(plan.cfg)[:12] != bytes(routed_sort_config(cfg))[:12] or (plan.cfg.align, plan.cfg.capacity) != (128, cfg.capacity):
+        raise EtrError(ERR_WORKSPACE, f"{where}: a plan made for another configuration")
+
+
 def routed_forward(cfg, X, topk_idx, weights, W1g, W1u, W2, buf: LayerBuffers, plan: SortBuffers, Y):
+    _routed_plan("etr_routed_forward", cfg, plan)
     _check(lib().etr_routed_forward(C.byref(cfg), _p(X), _p(topk_idx), _p(weights), _p(W1g), _p(W1u), _p(W2),
                                     C.byref(buf.c), C.byref(plan.c), _p(Y), _stream()), "etr_routed_forward")
 
 
 def routed_backward(cfg, weights, W1g, W1u, W2, dY, buf: LayerBuffers, plan: SortBuffers, dX, dweights, dW1g, dW1u, dW2):
+    _routed_plan("etr_routed_backward", cfg, plan)
     _check(lib().etr_routed_backward(C.byref(cfg), _p(weights), _p(W1g), _p(W1u), _p(W2), _p(dY), C.byref(buf.c),
                                      C.byref(plan.c), _p(dX), _p(dweights), _p(dW1g), _p(dW1u), _p(dW2), _stream()),
            "etr_routed_backward")
@@ -540,6 +553,7 @@ class BlockBuffers:
     def __init__(self, ncfg: NormConfig, device="cuda"):
         n = C.c_size_t(0)
         _check(lib().etr_block_bind(C.byref(ncfg), None, C.c_size_t(0), None, C.byref(n)), "etr_block_bind")
+        self.made = ncfg.T, ncfg.d, ncfg.dtype
         self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         base = (self.block.data_ptr() + 255) // 256 * 256
         self.c = BlockBuffersC()
@@ -551,13 +565,20 @@ class BlockBuffers:
             setattr(self, name, self.block[off:off + size].view(act).view(rows))
 
 
+def _block_buffers(where, ncfg, bb):
+    if bb.made != (ncfg.T, ncfg.d, ncfg.dtype):
+        raise EtrError(ERR_WORKSPACE, f"{where}: block buffers made for another configuration")
+
+
 def block_forward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, buf: LayerBuffers, bb: BlockBuffers, Xo):
+    _block_buffers("etr_block_forward", ncfg, bb)
     _check(lib().etr_block_forward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
                                    _p(W1u), _p(W2), C.byref(buf.c), C.byref(bb.c), _p(Xo), _stream()), "etr_block_forward")
 
 
 def block_backward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, dXo, buf: LayerBuffers, bb: BlockBuffers, dX, dw_pre,
                    dw_post, dgate, dR, dW1g, dW1u, dW2):
+    _block_buffers("etr_block_backward", ncfg, bb)
     _check(lib().etr_block_backward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
                                     _p(W1u), _p(W2), _p(dXo), C.byref(buf.c), C.byref(bb.c), _p(dX), _p(dw_pre),
                                     _p(dw_post), _p(dgate), _p(dR), _p(dW1g), _p(dW1u), _p(dW2), _stream()),

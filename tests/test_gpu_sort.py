@@ -224,4 +224,13 @@ def test_calls_are_refused_before_a_launch():
     with pytest.raises(etr.EtrError) as e:
         etr.sort(cfg, torch.zeros(10, 2, dtype=torch.int64, device="cuda"), buf)
     assert e.value.code == etr.ERR_ARG
+    for other in (dict(T=9), dict(k=3), dict(E=5), dict(align=8), dict(align=128, capacity=8)):       # a plan of another configuration
+        c = etr.make_sort_config(**dict(dict(T=10, k=2, E=4, d=64, dtype=etr.BF16), **other))
+        with pytest.raises(etr.EtrError) as e:
+            etr.sort(c, torch.zeros(c.T, c.k, dtype=torch.int32, device="cuda"), buf)
+        assert e.value.code == etr.ERR_WORKSPACE
+    cfg.T = 11                                             # the buffers keep the configuration they were made for
+    with pytest.raises(etr.EtrError) as e:
+        etr.sort(cfg, torch.zeros(11, 2, dtype=torch.int32, device="cuda"), buf)
+    assert e.value.code == etr.ERR_WORKSPACE
     assert etr.launch_count() == n0

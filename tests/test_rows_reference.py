@@ -216,6 +216,10 @@ def test_binding_refuses_what_addresses_do_not_show():
             etr.prenorm(cfg, bad, None, x)
         assert e.value.code == etr.ERR_ARG
     plan = etr.SortBuffers(sort_cfg(), device="cpu")
+    for other in (dict(T=5), dict(k=1), dict(E=4), dict(align=2), dict(align=128, capacity=4)):
+        with pytest.raises(etr.EtrError) as e:
+            etr.sort_rows(sort_cfg(**other), x, plan, x)          # a plan of another configuration
+        assert e.value.code in (etr.ERR_WORKSPACE, etr.ERR_ARG)
     with pytest.raises(etr.EtrError) as e:
         etr.sort(plan.cfg, torch.zeros(4, 2, dtype=torch.int32), plan)
     assert e.value.code == etr.ERR_ARG
