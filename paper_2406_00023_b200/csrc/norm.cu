@@ -151,7 +151,9 @@ struct RowRing {
 // pieces a thread, 512 with 128 (the join's spills at 112).
 constexpr int norm_bwd_threads(bool join, int nv) { return join || nv > 2 ? 512 : 576; }
 
-// Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.
+// Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.  HBM-bound: bf16, prenorm of
+// 65536 x 4096 164 us (the copy rate), join of 65536 x 4096 347 us (94 %), of 6113 x 2048 17.8 us (86 %: seven tiles a block,
+// ramp and tail); a few rows cost a launch (64 x 4096: join 2.5 us in a graph).
 template <class T, int NV, bool RING, bool JOIN, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 norm_fwd_kernel(const NormArgs p, const RowShape sh) {
@@ -247,7 +249,8 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   }
 }
 
-// Backward.  Blocks walk tiles of rpb rows in strides, a thread always on the same columns, so the gains' gradients add up in
+// Backward, HBM-bound: bf16, join of 65536 x 4096 491 us (the copy rate), prenorm of 16384 x 2048 45 us (90 %, 3 us of them
+// norm_dw_kernel).  Blocks walk tiles of rpb rows in strides, a thread always on the same columns, so the gains' gradients add up in
 // registers; a block leaves one row of partial sums per gain, which norm_dw_kernel adds in order.
 // JOIN false: prenorm (Xo_in is its input X, dXo the gradient that comes along the residual, may be NULL; no y).
 // The factors that are the same for a whole row (r_o, r_y, gate, a, b) are taken out of the sums over it:

@@ -203,7 +203,8 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
       if (lo + lane < lo4) row_token[lo + lane] = -1;
       if (hi4 + lane < hi) row_token[hi4 + lane] = -1;
     }
-    for (int r = lo4 + 4 * (lane + 32 * (parts > 1 ? share : 0)); r < hi4; r += 128 * parts) *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
+    for (int r = lo4 + 4 * (lane + 32 * (parts > 1 ? share : 0)); r < hi4; r += 128 * parts)
+      *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
   }
   if (blockIdx.x == 0 && tid == 0) {
     int end = 0, all = 0, with = 0;
@@ -225,9 +226,10 @@ __device__ __forceinline__ void zero_pad_rows(uint4* rows, int nv, const int32_t
   for (size_t v = share * 256 + threadIdx.x; v < n; v += shares * 256) dst[v] = make_uint4(0, 0, 0, 0);
 }
 
-// Xs[pos[t][j]] = X[t].  Token-major, so that a token is read once however many experts it has.  X is a flat run of
-// 16-byte pieces; a thread takes U of them, and asks for the rows of AHEAD pairs of each (four, or k where
-// that is fewer) before it stores.
+// Xs[pos[t][j]] = X[t].  Token-major, so that a token is read once however many experts it has: HBM-bound, 65536 x 4096 bf16, k = 2
+// 245 us, which is the copy rate (row-major, a token once per expert, would move a third more).  X is a flat run of 16-byte
+// pieces; a thread takes U of them, and asks for the rows of AHEAD pairs of each (four, or k where that is fewer) before
+// it stores (rows asked for one by one: 250 us, and 64 x 1024 2.5 us against 1.6).
 constexpr int SORT_PIECES = 4;                   // U of batches that fill the SMs; 1 for shorter ones
 template <int U, int AHEAD>
 __global__ void __launch_bounds__(256)
@@ -347,7 +349,8 @@ unsort_few_kernel(const uint4* rows, const float* w, const int32_t* pos, uint4* 
 }
 
 // dO[pos[t][j]] = w[t][j] dY[t], dw[t][j] = <dY[t], O[pos[t][j]]>; L lanes per pair (a warp, or the power of two that holds a
-// short row).  The pairs of a token are neighbours, so its dY comes from HBM once.
+// short row).  The pairs of a token are neighbours, so its dY comes from HBM once.  HBM-bound: 65536 x 4096 bf16, k = 2 400 us, the copy
+// rate.
 template <class T>
 __global__ void __launch_bounds__(256)
 unsort_bwd_kernel(const uint4* dY, const uint4* O, const float* w, const int32_t* pos, const int32_t* counts, const int32_t* offsets,
@@ -477,7 +480,7 @@ static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* 
   if (p == nullptr || p->counts == nullptr || p->offsets == nullptr || p->totals == nullptr || p->scratch == nullptr) return ETR_ERR_ARG;
   const bool rows = sort_rows_bound(c) > 0, some = c->T > 0;
   if ((rows && p->row_token == nullptr) || (some && p->pos == nullptr)) return ETR_ERR_ARG;
-  for (const void* q : {(const void*)p->counts, (const void*)p->offsets, (const void*)p->totals, (const void*)p->row_token, (const void*)p->pos, (const void*)p->scratch})
+  for (const int32_t* q : {p->counts, p->offsets, p->totals, p->row_token, p->pos, p->scratch})
     if (!aligned16(q)) return ETR_ERR_ALIGN;
   if (!some) return ETR_OK;                  // nothing is read or written through them
   for (const void* q : more) {
@@ -555,13 +558,15 @@ static etr_status sort_pass(int which, const etr_sort_config* c, const etr_sort_
   switch (which) {
     case 0:
       ETR_TIME_BEGIN("sort_rows_kernel");
-      launch_kernel(!full ? sort_rows_kernel<1, 4> : c->k == 1 ? sort_rows_kernel<SORT_PIECES, 1> : c->k == 2 ? sort_rows_kernel<SORT_PIECES, 2> : sort_rows_kernel<SORT_PIECES, 4>, (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, p->pos, p->counts, p->offsets, (uint4*)out, n,
-                    nv, c->k, c->align, pad);
+      launch_kernel(!full ? sort_rows_kernel<1, 4> : c->k == 1 ? sort_rows_kernel<SORT_PIECES, 1> : c->k == 2 ? sort_rows_kernel<SORT_PIECES, 2>
+                                                                                                 : sort_rows_kernel<SORT_PIECES, 4>,
+                    (unsigned)(blocks + pad), 256, 0, st, 1, (const uint4*)a, p->pos, p->counts, p->offsets, (uint4*)out, n, nv, c->k, c->align, pad);
       break;
     case 1:
       ETR_TIME_BEGIN("unsort_kernel");
       if (few)
-        launch_kernel(c->k == 1 ? unsort_few_kernel<T, 1> : c->k == 2 ? unsort_few_kernel<T, 2> : c->k == 3 ? unsort_few_kernel<T, 3> : unsort_few_kernel<T, 4>,
+        launch_kernel(c->k == 1 ? unsort_few_kernel<T, 1> : c->k == 2 ? unsort_few_kernel<T, 2> : c->k == 3 ? unsort_few_kernel<T, 3>
+                                                                                                 : unsort_few_kernel<T, 4>,
                       (unsigned)blocks, UNSORT_THREADS, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv);
       else
         launch_kernel(unsort_kernel<T>, (unsigned)blocks, UNSORT_THREADS, 0, st, 1, (const uint4*)a, w, p->pos, (uint4*)out, n, nv, c->k);
