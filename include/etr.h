@@ -488,7 +488,7 @@ etr_status etr_routed_backward(const etr_config* cfg, const float* weights, cons
 
 /* Rows of d values (d % 8 == 0, d <= ETR_NORM_MAX_D) of `dtype`; gains, gates, 1/rms and their gradients fp32; pointers 16-byte
  * aligned.  r(x) = 1 / sqrt(mean x^2 + eps), eps > 0.  A NULL gain or gate means ones.  T = 0 writes zero weight gradients
- * and nothing else.  Values below 1e18 in size (their squares are summed in fp32).
+ * and nothing else.  Values and gradients below 1e17 in size (their squares and products are summed in fp32).
  * Xo may be X, and dX may be dXo or dres (the residual stream updated in place); no other output may overlap an input. */
 #define ETR_NORM_MAX_D 16384
 typedef struct etr_norm_config {

@@ -179,6 +179,24 @@ def test_small_values_keep_eps_in_charge():
         rr.assert_within(r, r_ref, r_bound, "rstd")
 
 
+@TYPES
+def test_values_up_to_the_documented_size(dtype):
+    """1e17 in the widest rows: the sum of the squares is half of what fp32 holds."""
+    T, d = 5, 16384
+    X, dN = ((torch.rand(T, d, device="cuda") * 2 - 1).mul_(9.9e16).to(dtype) for _ in range(2))
+    X[0] = 9.9e16
+    cfg = etr.make_norm_config(T=T, d=d, dtype=DT[dtype], eps=EPS)
+    N, r, dX, dw = nans(T, d, dtype=dtype), nans(T), nans(T, d, dtype=dtype), nans(d)
+    etr.prenorm(cfg, X, None, N, r)
+    (ref, bound), (r_ref, r_bound) = rr.prenorm(X, None, EPS, dtype)
+    rr.assert_within(N, ref, bound, "N")
+    rr.assert_within(r, r_ref, r_bound, "rstd")
+    etr.prenorm_bwd(cfg, dN, X, None, r, None, dX, dw, workspace(cfg))
+    x, g = rr.prenorm_bwd(dN, X, None, r, None, dtype)
+    rr.assert_within(dX, *x, "dX")
+    rr.assert_within(dw, *g, "dw")
+
+
 def test_captured_calls_and_another_stream():
     T, d = 300, 1024
     cfg = etr.make_norm_config(T=T, d=d, dtype=etr.BF16, eps=EPS, res_scale=A, branch_scale=B, post_norm=True)
