@@ -50,11 +50,12 @@ sort_count_kernel(const int32_t* ids, SortShape s, int32_t* __restrict__ part) {
 }
 
 // The plan.  Every warp owns a run of consecutive pairs and counts its ids per expert (shared memory); the warps' counts become
-// prefix sums within the CTA, through distributed shared memory across the cluster, and through `part` across the
-// clusters (nclusters > 1).  The row of a pair is then its expert's start, plus the pairs of earlier warps, plus those
-// before it in its own warp (one match over the warp's 32 ids a round).  No atomics decide an order, so the plan is
-// stable and the same every time.  Bound by the latency of that chain, so a run's first SORT_KEPT rounds of ids stay in
-// registers, loops over warps and CTAs are unrolled (their loads in flight together), and a short batch is one small CTA.
+// prefix sums within the CTA, across the cluster (every CTA writes its counts to all others' shared memory, so that one
+// barrier later all reads are local: 32768 pairs 5.6 us, 6.4 with counts read from there), and through `part` across the
+// clusters (nclusters > 1).  The row of a pair is then its expert's start, plus the pairs of earlier warps, plus those before
+// it in its own warp (one match over the warp's 32 ids a round).  No atomics decide an order, so the plan is stable and the
+// same every time.  Bound by the latency of that chain, so a run's first SORT_KEPT rounds of ids stay in registers, loops over
+// warps and CTAs are unrolled (their loads in flight together), and a short batch is one small CTA (64 x 2 ids 2.7 us).
 constexpr int SORT_KEPT = 4;
 __global__ void __launch_bounds__(SORT_WARPS * 32)
 sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclusters, int32_t* __restrict__ counts,
@@ -66,19 +67,20 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
   const int threads = blockDim.x, warps = threads >> 5, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int ncta = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), my_cluster = blockIdx.x / ncta;
   int* wc = sm;                                  // [warps][E] pairs of this warp, then of the warps before it
-  int* mine = wc + warps * s.E;                  // [E] pairs of this CTA
-  int* start = mine + s.E;                       // [E] first row of the expert
+  int* cta = wc + warps * s.E;                   // [CTAs][E] pairs of each CTA of the cluster, written by that CTA
+  int* start = cta + ncta * s.E;                 // [E] first row of the expert
   int* before = start + s.E;                     // [E] pairs in the CTAs before this one
   int* used = before + s.E;                      // [E] pairs that get a row
   __shared__ int s_rows[SORT_WARPS], s_found[SORT_WARPS], s_kept[SORT_WARPS];
+  if (ncta > 1) cluster.barrier_arrive();        // this CTA runs: the others may write to its memory
   const long long beg = ((long long)blockIdx.x * warps + warp) * s.run;
   const int n = (int)max(0ll, min((long long)s.run, (long long)s.N - beg));
   int id[SORT_KEPT];
 #pragma unroll
   for (int u = 0; u < SORT_KEPT; ++u) id[u] = 32 * u + lane < n ? ids[beg + 32 * u + lane] : -1;
-  for (int i = tid; i < warps * s.E; i += threads) wc[i] = 0;
   int* cnt = wc + warp * s.E;
-  __syncthreads();
+  for (int e = lane; e < s.E; e += 32) cnt[e] = 0;
+  __syncwarp();
 #pragma unroll
   for (int u = 0; u < SORT_KEPT; ++u)
     if ((unsigned)id[u] < (unsigned)s.E) atomicAdd(&cnt[id[u]], 1);
@@ -88,6 +90,7 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     if ((unsigned)e < (unsigned)s.E) atomicAdd(&cnt[e], 1);
   }
   __syncthreads();
+  if (ncta > 1) cluster.barrier_wait();
   for (int e = tid; e < s.E; e += threads) {
     int c[SORT_WARPS], acc = 0;
 #pragma unroll
@@ -97,9 +100,13 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
       if (w < warps) wc[w * s.E + e] = acc;
       acc += c[w];
     }
-    mine[e] = acc;
+    if (ncta == 1) {
+      cta[e] = acc;
+    } else {
+      for (int q = 0; q < ncta; ++q) cluster.map_shared_rank(cta, q)[rank * s.E + e] = acc;
+    }
   }
-  if (ncta > 1) cluster.sync(); else __syncthreads();
+  if (ncta > 1) cluster.sync(); else __syncthreads();          // nothing goes to another CTA's memory behind this
   // Experts [2 tid, 2 tid + 2): pairs found, kept, and rows taken; the starts by a scan over the CTA's threads.
   int rows[2] = {0, 0}, found = 0, keeps = 0;
 #pragma unroll
@@ -107,16 +114,11 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     const int e = 2 * tid + u;
     if (e >= s.E) break;
     int all = 0, ahead = 0;
-    if (ncta == 1) {
-      all = mine[e];
-    } else {
-      for (int c0 = 0; c0 < ncta; c0 += 8)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const int v = c0 + c < ncta ? cluster.map_shared_rank(mine, c0 + c)[e] : 0;
-          all += v;
-          ahead += c0 + c < rank ? v : 0;
-        }
+#pragma unroll 8
+    for (int c = 0; c < ncta; ++c) {
+      const int v = cta[c * s.E + e];
+      all += v;
+      ahead += c < rank ? v : 0;
     }
     if (nclusters > 1) {
       all = 0;
@@ -135,7 +137,6 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     rows[u] = s.capacity ? s.stride : (keep + s.align - 1) / s.align * s.align;
     if (blockIdx.x == 0) counts[e] = keep;
   }
-  if (ncta > 1) cluster.barrier_arrive();        // done with the other CTAs' counts; waited for before leaving
   int inc = rows[0] + rows[1];
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -186,7 +187,7 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
         if (ok) r += before[e];
         const int row = ok && r < limit ? start[e] + r : -1;
         pos[beg + i] = row;
-        if (row >= 0) row_token[row] = (int)((beg + i) / s.k);
+        if (row >= 0) row_token[row] = (int)((unsigned)(beg + i) / (unsigned)s.k);
       }
     }
   }
@@ -212,7 +213,6 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
     offsets[s.E] = end;
     totals[0] = with; totals[1] = all - with; totals[2] = s.N - all; totals[3] = 0;
   }
-  if (ncta > 1) cluster.barrier_wait();          // no CTA leaves while another may still read its counts
 }
 
 // Pad rows (behind an expert's last row, up to the next multiple of `align`) are zeros.  The first blocks of a row pass, one
@@ -506,11 +506,11 @@ static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? pad
 
 // One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 16 of 16 warps (an opt-in size); longer batches take up to
 // 18 clusters of 8, and a launch before that counts the clusters' pairs.  Measured, a plan by itself: 32768 pairs of 32
-// experts 6.4 us in one cluster of 16, 8.4 of 8, 10 with the count; 65536 of 128 9.9 in one, 9.7 with the count; 131072 of 64
-// 14.4 and 10.3.
+// experts 5.6 us in one cluster of 16 (7.6 of 8, 9.5 with the count, before those counts were written instead of read); 65536 of
+// 128 8.9 in one; 131072 of 64 9.4 with the count (14 without), 524288 16.
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0}, wide{0};
-  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + 4) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + SORT_ALONE + 3) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
   if (!ensure_wide_cluster(sort_plan_kernel, wide)) return ETR_ERR_CUDA;
   SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c), 0};
   const int cta = SORT_WARPS * SORT_RUN;
@@ -531,7 +531,7 @@ static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, cons
     launch_kernel(sort_count_kernel, nclusters * SORT_CLUSTER, SORT_WARPS * 32, (size_t)c->E * 4, st, SORT_CLUSTER, ids, s, p->scratch);
     ETR_LAUNCH_CHECK();
   }
-  const size_t smem = (size_t)(warps + 4) * c->E * 4;
+  const size_t smem = (size_t)(warps + ncta + 3) * c->E * 4;
   ETR_TIME_BEGIN("sort_plan_kernel");
   launch_kernel(sort_plan_kernel, nclusters * ncta, warps * 32, smem, st, ncta, ids, s, (const int32_t*)p->scratch, nclusters, p->counts,
                 p->offsets, p->totals, p->row_token, p->pos);
