@@ -306,3 +306,52 @@ def test_captured_block_follows_its_inputs():
     calls()
     torch.cuda.synchronize()
     assert torch.equal(Xo, replayed[0]) and torch.equal(Y, replayed[1])
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with buffers of their own, interleaved without a wait between them: the bits of either alone."""
+    T, d, E, k = 5000, 1024, 48, 3
+    g = torch.Generator(device="cuda").manual_seed(6)
+    sc = etr.make_sort_config(T=T, k=k, E=E, d=d, dtype=etr.BF16, align=8)
+    nc = etr.make_norm_config(T=T, d=d, dtype=etr.BF16, eps=EPS, post_norm=True)
+    sets = []
+    for _ in range(2):
+        x = dict(ids=torch.randint(0, E, (T, k), generator=g, device="cuda", dtype=torch.int32), w=torch.rand(T, k, generator=g, device="cuda"),
+                 gain=torch.rand(d, generator=g, device="cuda"), gate=torch.rand(T, generator=g, device="cuda"))
+        for n in ("X", "dY", "dX"):
+            x[n] = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+        sets.append(x)
+
+    def state():
+        plan = etr.SortBuffers(sc)
+        rows = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")                            # noqa: E731
+        return dict(plan=plan, N=rows(T, d), Xs=rows(plan.n_rows, d), Y=rows(T, d), Xo=rows(T, d), dYo=rows(T, d), dXo=rows(T, d),
+                    dO=rows(plan.n_rows, d), dw=torch.zeros(T, k, device="cuda"), r=torch.zeros(T, device="cuda"), ry=torch.zeros(T, device="cuda"),
+                    dgain=torch.zeros(d, device="cuda"), ws=torch.empty(etr.norm_workspace_bytes(nc), dtype=torch.uint8, device="cuda"))
+
+    def step(x, s):
+        etr.prenorm(nc, x["X"], x["gain"], s["N"], s["r"])
+        etr.sort(sc, x["ids"], s["plan"])
+        etr.sort_rows(sc, s["N"], s["plan"], s["Xs"])
+        etr.unsort_rows(sc, s["Xs"], x["w"], s["plan"], s["Y"])
+        etr.join(nc, x["X"], s["Y"], x["gain"], x["gate"], None, s["Xo"], None, s["ry"])
+        etr.join_bwd(nc, x["dX"], None, s["Y"], None, x["gain"], x["gate"], None, s["ry"], None, s["dXo"], s["dYo"], s["dgain"], None, None, s["ws"])
+        etr.unsort_rows_bwd(sc, s["dYo"], s["Xs"], x["w"], s["plan"], s["dO"], s["dw"])
+
+    names = ("N", "Xs", "Y", "Xo", "dYo", "dXo", "dO", "dw", "dgain")
+    alone = []
+    for x in sets:
+        s = state()
+        step(x, s)
+        torch.cuda.synchronize()
+        alone.append({n: s[n].clone() for n in names})
+    both, streams = [state(), state()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, s, stream in zip(sets, both, streams):
+            with torch.cuda.stream(stream):
+                step(x, s)
+    torch.cuda.synchronize()
+    for s, ref in zip(both, alone):
+        for n in names:
+            assert torch.equal(s[n], ref[n]), n
