@@ -70,7 +70,8 @@ etr_status call(void* fn, int n, const void* c, void* const* a, void* st) {
 }
 
 // run(op, config address, device, arguments...): 0, or (status, what was wrong).  Plans are addresses of PlanFor; `device` is
-// the one that the plan's memory is on, -1 where there is no plan.  Nothing here allocates or waits.
+// the one that the plan's memory is on (-1: not a GPU), and -1 where the operator takes no plan.  The plan is looked over
+// before the tensors: the kernels write through its addresses.  Nothing here allocates or waits.
 PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   try {
     const long i = nargs >= 3 ? PyLong_AsLong(args[0]) : -1;
@@ -88,15 +89,18 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const auto act = (op.sort ? s->dtype : m->dtype) == ETR_BF16 ? at::kBFloat16 : at::kFloat;
     void* a[15];
     for (int j = 0; j < op.n; ++j) {
+      const Arg& w = op.arg[j];
+      if (w.kind != PLAN) continue;
+      auto* p = static_cast<PlanFor*>(PyLong_AsVoidPtr(args[3 + j]));
+      if (PyErr_Occurred()) return nullptr;
+      if (p == nullptr || !p->fits(*s)) return refuse(ETR_ERR_WORKSPACE, op, w, "made for another configuration");
+      if (device < 0) return refuse(ETR_ERR_ARG, op, w, "not on a CUDA device");
+      a[j] = &p->plan;
+    }
+    for (int j = 0; j < op.n; ++j) {
       PyObject* o = args[3 + j];
       const Arg& w = op.arg[j];
-      if (w.kind == PLAN) {
-        auto* p = static_cast<PlanFor*>(PyLong_AsVoidPtr(o));
-        if (PyErr_Occurred()) return nullptr;
-        if (p == nullptr || !p->fits(*s)) return refuse(ETR_ERR_WORKSPACE, op, w, "made for another configuration");
-        a[j] = &p->plan;
-        continue;
-      }
+      if (w.kind == PLAN) continue;
       if (o == Py_None) {
         if (!w.optional) return refuse(ETR_ERR_ARG, op, w, "a tensor is wanted");
         a[j] = nullptr;

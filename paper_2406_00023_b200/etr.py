@@ -528,6 +528,8 @@ def routed_sort_config(cfg: Config) -> SortConfig:
 def _routed_plan(where, cfg, plan):
     if bytes(plan.cfg)[:12] != bytes(routed_sort_config(cfg))[:12] or (plan.cfg.align, plan.cfg.capacity) != (128, cfg.capacity):
         raise EtrError(ERR_WORKSPACE, f"{where}: a plan made for another configuration")
+    if plan.device < 0:
+        raise EtrError(ERR_ARG, f"{where}: plan: not on a CUDA device")
 
 
 def routed_forward(cfg, X, topk_idx, weights, W1g, W1u, W2, buf: LayerBuffers, plan: SortBuffers, Y):
