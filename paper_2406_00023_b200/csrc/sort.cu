@@ -204,7 +204,8 @@ sort_plan_kernel(const int32_t* ids, SortShape s, const int32_t* part, int nclus
       if (lo + lane < lo4) row_token[lo + lane] = -1;
       if (hi4 + lane < hi) row_token[hi4 + lane] = -1;
     }
-    for (int r = lo4 + 4 * (lane + 32 * (parts > 1 ? share : 0)); r < hi4; r += 128 * parts)
+    // in 64 bits: a lane's first row and its step past the last one lie up to 128 * 2304 rows behind hi4, which may be near 2^31
+    for (long long r = lo4 + 4ll * (lane + 32 * (parts > 1 ? share : 0)); r < hi4; r += 128ll * parts)
       *reinterpret_cast<int4*>(row_token + r) = make_int4(-1, -1, -1, -1);
   }
   if (blockIdx.x == 0 && tid == 0) {
