@@ -476,7 +476,8 @@ etr_status etr_unsort_rows_bwd(const etr_sort_config* cfg, const void* dY, const
  * etr_unsort_rows_bwd, etr_expert_ffn_bwd, etr_sort_rows_bwd on the buffers and the plan that the forward call filled.
  * cfg is the layer's (k <= ETR_SORT_MAX_K); its D, mode, step, adaptive, gate, threshold and fuse members are not used.
  * buf->stats is cleared, and afterwards holds only the error word.  plan: etr_sort_plan_bind of
- * {T, k, E, d, dtype, 128, capacity}.  With capacity = T nothing is dropped whatever the choice. */
+ * {T, k, E, d, dtype, 128, capacity}.  Nothing is dropped with capacity = T where no token names an expert twice, and with
+ * capacity = k T whatever the choice; plan->totals[1] counts the pairs that were. */
 etr_status etr_routed_forward(const etr_config* cfg, const void* X, const int32_t* topk_idx, const float* weights,
                               const void* W1g, const void* W1u, const void* W2, const etr_buffers* buf,
                               const etr_sort_plan* plan, void* Y, void* stream);
