@@ -1,4 +1,5 @@
-"""Binding of libetr (include/etr.h): ctypes, and csrc/args.cpp for the row operators.  Argument marshalling only.
+"""Binding of libetr (include/etr.h): ctypes, and csrc/args.cpp for the row operators and the calls composed of them.
+Argument marshalling only.
 
 Tensors are torch CUDA tensors used as plain device memory; the current torch stream is
 passed to every call.  The library is loaded from this package's directory and loading
@@ -182,6 +183,11 @@ def workspace_bytes(cfg: Config) -> int:
     return n.value
 
 
+class LayerBuffersFor(C.Structure):
+    """Buffers, the configuration that their memory was carved for, and the device that it is on."""
+    _fields_ = [("buf", Buffers), ("made", Config), ("device", C.c_int32)]
+
+
 class LayerBuffers:
     """One device block carved by etr_buffers_bind, with typed tensor views of each member."""
 
@@ -193,7 +199,8 @@ class LayerBuffers:
         self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         base = (self.block.data_ptr() + 255) // 256 * 256
         self._base_off = base - self.block.data_ptr()
-        self.c = Buffers()
+        self._for = LayerBuffersFor(made=cfg, device=self.block.get_device())       # a copy of cfg; -1: not on a GPU
+        self.c, self.ptr = self._for.buf, C.addressof(self._for)
         _check(lib().etr_buffers_bind(C.byref(cfg), int(host_staging), C.c_void_p(base),
                                       C.c_size_t(n.value), C.byref(self.c)), "etr_buffers_bind")
         T, E, d, h, k = cfg.T, cfg.E, cfg.d, cfg.h, cfg.k
@@ -393,8 +400,8 @@ class SortPlan(C.Structure):
 
 
 class SortPlanFor(C.Structure):
-    """A plan and the configuration that its memory was carved for."""
-    _fields_ = [("plan", SortPlan), ("made", SortConfig)]
+    """A plan, the configuration that its memory was carved for, and the device that it is on."""
+    _fields_ = [("plan", SortPlan), ("made", SortConfig), ("device", C.c_int32)]
 
 
 SORT_MAX_K, SORT_MAX_E, NORM_MAX_D = 32, 1024, 16384
@@ -421,7 +428,8 @@ class SortBuffers:
         self.n_rows = sort_n_rows(cfg)
         self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         base = (self.block.data_ptr() + 255) // 256 * 256
-        both = SortPlanFor(made=cfg)               # a copy of cfg
+        self.device = self.block.get_device()          # -1: not on a GPU, which every call refuses
+        both = SortPlanFor(made=cfg, device=self.device)               # a copy of cfg
         self.c, self.cfg = both.plan, both.made
         _check(lib().etr_sort_plan_bind(C.byref(cfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_sort_plan_bind")
         for name, shape in (("counts", (cfg.E,)), ("offsets", (cfg.E + 1,)), ("totals", (4,)), ("row_token", (self.n_rows,)),
@@ -431,13 +439,13 @@ class SortBuffers:
                 count *= m
             setattr(self, name, self.block[off:off + 4 * count].view(torch.int32).view(shape))
         self._both, self.ptr = both, C.addressof(both)
-        self.device = self.block.get_device()          # -1: not on a GPU, which every call refuses
 
 
-# The row operators go through csrc/args.cpp, which looks every tensor over (type, place, order, size: refusals are EtrError) and
-# calls the C function on the current stream: 0.5 to 1 us a call instead of 5 to 10 through ctypes.
+# The row operators and the calls composed of them go through csrc/args.cpp, which looks every tensor and buffer over (type, place,
+# order, size: refusals are EtrError) and calls the C function on the current stream: 0.5 to 1 us a call instead of 5 to 10
+# through ctypes.
 _ROW_OPS = ("etr_sort", "etr_sort_rows", "etr_sort_rows_bwd", "etr_unsort_rows", "etr_unsort_rows_bwd", "etr_prenorm", "etr_prenorm_bwd",
-            "etr_join", "etr_join_bwd")
+            "etr_join", "etr_join_bwd", "etr_routed_forward", "etr_routed_backward", "etr_block_forward", "etr_block_backward")
 
 
 def _load_and_run(*args):
@@ -448,7 +456,7 @@ def _load_and_run(*args):
         raise RuntimeError("_args.so not built; run `python -m paper_2406_00023_b200.build`") from e
     assert _args.names == _ROW_OPS
     l = lib()
-    _args.bind(*[C.cast(getattr(l, n), C.c_void_p).value for n in _ROW_OPS + ("etr_sort_n_rows", "etr_norm_workspace_bytes")])
+    _args.bind(*[C.cast(getattr(l, n), C.c_void_p).value for n in _ROW_OPS + ("etr_sort_n_rows", "etr_norm_workspace_bytes", "etr_validate")])
     _run = _args.run
     return _run(*args)
 
@@ -463,23 +471,23 @@ def _row_op(*args):
 
 
 def sort(cfg, topk_idx, plan: SortBuffers):
-    _row_op(0, C.addressof(cfg), plan.device, topk_idx, plan.ptr)
+    _row_op(0, C.addressof(cfg), topk_idx, plan.ptr)
 
 
 def sort_rows(cfg, X, plan: SortBuffers, Xs):
-    _row_op(1, C.addressof(cfg), plan.device, X, plan.ptr, Xs)
+    _row_op(1, C.addressof(cfg), X, plan.ptr, Xs)
 
 
 def sort_rows_bwd(cfg, dXs, plan: SortBuffers, dX):
-    _row_op(2, C.addressof(cfg), plan.device, dXs, plan.ptr, dX)
+    _row_op(2, C.addressof(cfg), dXs, plan.ptr, dX)
 
 
 def unsort_rows(cfg, O, weights, plan: SortBuffers, Y):
-    _row_op(3, C.addressof(cfg), plan.device, O, weights, plan.ptr, Y)
+    _row_op(3, C.addressof(cfg), O, weights, plan.ptr, Y)
 
 
 def unsort_rows_bwd(cfg, dY, O, weights, plan: SortBuffers, dO, dweights):
-    _row_op(4, C.addressof(cfg), plan.device, dY, O, weights, plan.ptr, dO, dweights)
+    _row_op(4, C.addressof(cfg), dY, O, weights, plan.ptr, dO, dweights)
 
 
 # ---- the norm before a block and the join behind it -------------------------------------------------
@@ -504,19 +512,19 @@ def norm_workspace_bytes(cfg: NormConfig) -> int:
 
 
 def prenorm(cfg, X, w, N, rstd=None):
-    _row_op(5, C.addressof(cfg), -1, X, w, N, rstd)
+    _row_op(5, C.addressof(cfg), X, w, N, rstd)
 
 
 def prenorm_bwd(cfg, dN, X, w, rstd, dres, dX, dw, ws):
-    _row_op(6, C.addressof(cfg), -1, dN, X, w, rstd, dres, dX, dw, ws)
+    _row_op(6, C.addressof(cfg), dN, X, w, rstd, dres, dX, dw, ws)
 
 
 def join(cfg, X, Y, w_post, gate, w_next, Xo, N, rstd_y=None, rstd_o=None):
-    _row_op(7, C.addressof(cfg), -1, X, Y, w_post, gate, w_next, Xo, N, rstd_y, rstd_o)
+    _row_op(7, C.addressof(cfg), X, Y, w_post, gate, w_next, Xo, N, rstd_y, rstd_o)
 
 
 def join_bwd(cfg, dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws):
-    _row_op(8, C.addressof(cfg), -1, dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws)
+    _row_op(8, C.addressof(cfg), dXo, dN, Y, Xo, w_post, gate, w_next, rstd_y, rstd_o, dX, dY, dw_post, dgate, dw_next, ws)
 
 
 # ---- the layer's experts under a given choice; norm, layer and join as one call --------------------------
@@ -525,28 +533,21 @@ def routed_sort_config(cfg: Config) -> SortConfig:
     return make_sort_config(T=cfg.T, k=cfg.k, E=cfg.E, d=cfg.d, dtype=cfg.dtype, align=128, capacity=cfg.capacity)
 
 
-def _routed_plan(where, cfg, plan):
-    if bytes(plan.cfg)[:12] != bytes(routed_sort_config(cfg))[:12] or (plan.cfg.align, plan.cfg.capacity) != (128, cfg.capacity):
-        raise EtrError(ERR_WORKSPACE, f"{where}: a plan made for another configuration")
-    if plan.device < 0:
-        raise EtrError(ERR_ARG, f"{where}: plan: not on a CUDA device")
-
-
 def routed_forward(cfg, X, topk_idx, weights, W1g, W1u, W2, buf: LayerBuffers, plan: SortBuffers, Y):
-    _routed_plan("etr_routed_forward", cfg, plan)
-    _check(lib().etr_routed_forward(C.byref(cfg), _p(X), _p(topk_idx), _p(weights), _p(W1g), _p(W1u), _p(W2),
-                                    C.byref(buf.c), C.byref(plan.c), _p(Y), _stream()), "etr_routed_forward")
+    _row_op(9, C.addressof(cfg), X, topk_idx, weights, W1g, W1u, W2, buf.ptr, plan.ptr, Y)
 
 
 def routed_backward(cfg, weights, W1g, W1u, W2, dY, buf: LayerBuffers, plan: SortBuffers, dX, dweights, dW1g, dW1u, dW2):
-    _routed_plan("etr_routed_backward", cfg, plan)
-    _check(lib().etr_routed_backward(C.byref(cfg), _p(weights), _p(W1g), _p(W1u), _p(W2), _p(dY), C.byref(buf.c),
-                                     C.byref(plan.c), _p(dX), _p(dweights), _p(dW1g), _p(dW1u), _p(dW2), _stream()),
-           "etr_routed_backward")
+    _row_op(10, C.addressof(cfg), weights, W1g, W1u, W2, dY, buf.ptr, plan.ptr, dX, dweights, dW1g, dW1u, dW2)
 
 
 class BlockBuffersC(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("N", "Y", "dN", "dY", "rstd_x", "rstd_y", "ws")]
+
+
+class BlockBuffersFor(C.Structure):
+    """Block buffers, the configuration that their memory was carved for, and the device that it is on."""
+    _fields_ = [("buf", BlockBuffersC), ("made", NormConfig), ("device", C.c_int32)]
 
 
 class BlockBuffers:
@@ -555,10 +556,10 @@ class BlockBuffers:
     def __init__(self, ncfg: NormConfig, device="cuda"):
         n = C.c_size_t(0)
         _check(lib().etr_block_bind(C.byref(ncfg), None, C.c_size_t(0), None, C.byref(n)), "etr_block_bind")
-        self.made = ncfg.T, ncfg.d, ncfg.dtype
         self.block = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         base = (self.block.data_ptr() + 255) // 256 * 256
-        self.c = BlockBuffersC()
+        self._for = BlockBuffersFor(made=ncfg, device=self.block.get_device())       # a copy of ncfg; -1: not on a GPU
+        self.c, self.ptr = self._for.buf, C.addressof(self._for)
         _check(lib().etr_block_bind(C.byref(ncfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_block_bind")
         act, rows = torch_dtype(ncfg), (ncfg.T, ncfg.d)
         for name in ("N", "Y", "dN", "dY"):
@@ -567,21 +568,11 @@ class BlockBuffers:
             setattr(self, name, self.block[off:off + size].view(act).view(rows))
 
 
-def _block_buffers(where, ncfg, bb):
-    if bb.made != (ncfg.T, ncfg.d, ncfg.dtype):
-        raise EtrError(ERR_WORKSPACE, f"{where}: block buffers made for another configuration")
-
-
 def block_forward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, buf: LayerBuffers, bb: BlockBuffers, Xo):
-    _block_buffers("etr_block_forward", ncfg, bb)
-    _check(lib().etr_block_forward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
-                                   _p(W1u), _p(W2), C.byref(buf.c), C.byref(bb.c), _p(Xo), _stream()), "etr_block_forward")
+    _row_op(11, C.addressof(cfg), C.addressof(ncfg), X, w_pre, w_post, gate, R, W1g, W1u, W2, buf.ptr, bb.ptr, Xo)
 
 
 def block_backward(cfg, ncfg, X, w_pre, w_post, gate, R, W1g, W1u, W2, dXo, buf: LayerBuffers, bb: BlockBuffers, dX, dw_pre,
                    dw_post, dgate, dR, dW1g, dW1u, dW2):
-    _block_buffers("etr_block_backward", ncfg, bb)
-    _check(lib().etr_block_backward(C.byref(cfg), C.byref(ncfg), _p(X), _p(w_pre), _p(w_post), _p(gate), _p(R), _p(W1g),
-                                    _p(W1u), _p(W2), _p(dXo), C.byref(buf.c), C.byref(bb.c), _p(dX), _p(dw_pre),
-                                    _p(dw_post), _p(dgate), _p(dR), _p(dW1g), _p(dW1u), _p(dW2), _stream()),
-           "etr_block_backward")
+    _row_op(12, C.addressof(cfg), C.addressof(ncfg), X, w_pre, w_post, gate, R, W1g, W1u, W2, dXo, buf.ptr, bb.ptr, dX, dw_pre, dw_post, dgate,
+            dR, dW1g, dW1u, dW2)

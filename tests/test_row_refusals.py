@@ -28,11 +28,6 @@ def test_a_plan_that_is_not_on_a_gpu_is_refused_for_itself():
     assert plan.device == -1
     for name, call in sort_calls(cfg, plan).items():
         refused(lambda: call(cfg), etr.ERR_ARG, name, "plan: not on a CUDA device")
-    layer = etr.make_config(T=4, d=64, D=8, E=4, k=2, h=64, capacity=4, dtype=etr.BF16)
-    plan, buf = etr.SortBuffers(etr.routed_sort_config(layer), device="cpu"), etr.LayerBuffers(layer, device="cpu")
-    refused(lambda: etr.routed_forward(layer, None, None, None, None, None, None, buf, plan, None), etr.ERR_ARG, "plan: not on a CUDA device")
-    refused(lambda: etr.routed_backward(layer, None, None, None, None, None, buf, plan, None, None, None, None, None), etr.ERR_ARG,
-            "plan: not on a CUDA device")
 
 
 @pytest.mark.parametrize("other", [dict(T=5), dict(k=1), dict(E=4), dict(align=2), dict(align=128, capacity=4)], ids=str)
@@ -42,3 +37,69 @@ def test_a_plan_of_another_configuration_is_refused_for_that(other):
     cfg = etr.make_sort_config(**dict(made, **other))
     for name, call in sort_calls(plan.cfg, plan).items():
         refused(lambda: call(cfg), etr.ERR_WORKSPACE, name, "plan: made for another configuration")
+
+
+# ---- the composed calls ------------------------------------------------------------------------------
+LAYER = dict(T=4, d=64, D=8, E=4, k=2, h=64, capacity=4, dtype=etr.BF16)
+
+
+def composed_calls(buf, plan, bb):
+    """Every composed call under a given configuration, its tensors left out."""
+    return {"etr_routed_forward": lambda c, n: etr.routed_forward(c, *[None] * 6, buf, plan, None),
+            "etr_routed_backward": lambda c, n: etr.routed_backward(c, *[None] * 5, buf, plan, *[None] * 5),
+            "etr_block_forward": lambda c, n: etr.block_forward(c, n, *[None] * 8, buf, bb, None),
+            "etr_block_backward": lambda c, n: etr.block_backward(c, n, *[None] * 9, buf, bb, *[None] * 8)}
+
+
+def made(**kw):
+    cfg, device = etr.make_config(**dict(LAYER, **kw)), "cpu"
+    n = etr.make_norm_config(T=cfg.T, d=cfg.d, dtype=cfg.dtype)
+    return cfg, n, etr.LayerBuffers(cfg, device=device), etr.SortBuffers(etr.routed_sort_config(cfg), device=device), etr.BlockBuffers(n, device=device)
+
+
+def test_composed_calls_refuse_buffers_that_are_not_on_a_gpu():
+    cfg, n, buf, plan, bb = made()
+    for name, call in composed_calls(buf, plan, bb).items():
+        refused(lambda: call(cfg, n), etr.ERR_ARG, name, "buf: not on a CUDA device")
+        buf._for.device = 0                                  # the other handle is looked at as well
+        refused(lambda: call(cfg, n), etr.ERR_ARG, name, "plan: " if "routed" in name else "bb: ", "not on a CUDA device")
+        buf._for.device = -1
+
+
+@pytest.mark.parametrize("other", [dict(T=5), dict(k=1), dict(E=3), dict(capacity=200)], ids=str)
+def test_composed_calls_refuse_a_plan_of_another_configuration(other):
+    cfg, n, buf, _, bb = made()
+    plan = etr.SortBuffers(etr.routed_sort_config(etr.make_config(**dict(LAYER, **other))), device="cpu")
+    for name, call in composed_calls(buf, plan, bb).items():
+        if "routed" in name:
+            refused(lambda: call(cfg, n), etr.ERR_WORKSPACE, name, "plan: made for another configuration")
+
+
+@pytest.mark.parametrize("other, fits", [
+    (dict(T=3), False), (dict(E=3), False), (dict(d=32, D=4), False), (dict(h=32), False), (dict(k=1), False), (dict(capacity=0x80, E=3), False),
+    (dict(dtype=etr.BF16, h=8), False), (dict(T=5, E=5, k=3, d=128, h=128, capacity=300), True), (dict(dtype=etr.F32), True), (dict(), True)], ids=str)
+def test_composed_calls_refuse_buffers_of_a_smaller_layer(other, fits):
+    """Buffers of a larger one serve as they do for the layer's own calls: what is wrong then is that these are not on a GPU."""
+    small = etr.LayerBuffers(etr.make_config(**dict(LAYER, gemm_impl=etr.GEMM_SIMT, **other)), device="cpu")
+    cfg, n, _, plan, bb = made()
+    for name, call in composed_calls(small, plan, bb).items():
+        if fits:
+            refused(lambda: call(cfg, n), etr.ERR_ARG, name, "buf: not on a CUDA device")
+        else:
+            refused(lambda: call(cfg, n), etr.ERR_WORKSPACE, name, "buf: made for another configuration")
+
+
+@pytest.mark.parametrize("other", [dict(T=5), dict(d=128), dict(dtype=etr.F32)], ids=str)
+def test_composed_calls_refuse_block_buffers_of_another_configuration(other):
+    cfg, n, buf, plan, _ = made()
+    bb = etr.BlockBuffers(etr.make_norm_config(**dict(dict(T=4, d=64, dtype=etr.BF16), **other)), device="cpu")
+    for name, call in composed_calls(buf, plan, bb).items():
+        if "block" in name:
+            refused(lambda: call(cfg, n), etr.ERR_WORKSPACE, name, "bb: made for another configuration")
+
+
+def test_composed_calls_check_the_configuration_first():
+    cfg, n, buf, plan, bb = made()
+    for bad, code in ((dict(k=5), etr.ERR_SHAPE), (dict(h=0), etr.ERR_ARG), (dict(D=0), etr.ERR_ARG)):
+        for name, call in composed_calls(buf, plan, bb).items():
+            refused(lambda: call(etr.make_config(**dict(LAYER, **bad)), n), code, name)
