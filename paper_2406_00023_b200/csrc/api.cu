@@ -493,6 +493,19 @@ etr_status etr_layer_backward(const etr_config* c, const void* X, const float* R
                            b->dXp, dX, dR, b->ws, b->stats, (cudaStream_t)stream);
 }
 
+// What the layer calls read and write of their buffers, for the calls that launch something before them.
+static etr_status check_layer_buffers(const etr_config* c, const etr_buffers* b, bool backward) {
+  ETR_TRY(check_route(&b->route));
+  ETR_TRY(check_ptrs({b->delta, b->xnorm, b->rnorm, b->G, b->U, b->H, b->O, b->ws}));
+  if (!backward || use_tc(c)) ETR_TRY(check_ptrs({b->stats}));
+  if (!fuse_dispatch(c)) ETR_TRY(check_ptrs({b->Xp}));
+  if (c->gate_mode == ETR_GATE_SOFTMAX) ETR_TRY(check_ptrs({b->lse}));
+  if (!backward) return aligned16(b->Z) ? ETR_OK : ETR_ERR_ALIGN;
+  if (c->gate_mode == ETR_GATE_SOFTMAX) ETR_TRY(check_ptrs({b->ddelta}));
+  if (b->Z == nullptr) return ETR_ERR_ARG;              // the backward pass takes any float Z
+  return check_ptrs({b->dO, b->dG, b->dU, b->dXp, b->dgate});
+}
+
 // ---- the experts under the caller's own choice ---------------------------------------------------
 static etr_sort_config routed_sort_config(const etr_config* c) {
   return etr_sort_config{c->T, c->k, c->E, c->d, c->dtype, 128, c->capacity, 0};
@@ -514,7 +527,7 @@ etr_status etr_routed_forward(const etr_config* c, const void* X, const int32_t*
   ETR_TRY(check_ptrs({X, topk_idx, weights, W1g, W1u, W2, b->stats, b->Xp, b->G, b->U, b->H, b->O, b->ws, Y}));
   ETR_TRY(check_workspace(c, b, false, false));
   const etr_sort_config s = routed_sort_config(c);
-  ETR_TRY(etr_sort_validate(&s));
+  ETR_TRY(sort_check_plan(&s, plan));
   if (cudaMemsetAsync(b->stats, 0, sizeof(etr_stats), (cudaStream_t)stream) != cudaSuccess) return ETR_ERR_CUDA;
   ETR_TRY(etr_sort(&s, topk_idx, plan, stream));
   ETR_TRY(etr_sort_rows(&s, X, plan, b->Xp, stream));
@@ -532,6 +545,7 @@ etr_status etr_routed_backward(const etr_config* c, const float* weights, const 
                       dW1g, dW1u, dW2}));
   ETR_TRY(check_workspace(c, b, false, false));
   const etr_sort_config s = routed_sort_config(c);
+  ETR_TRY(sort_check_plan(&s, plan));
   ETR_TRY(etr_unsort_rows_bwd(&s, dY, b->O, weights, plan, b->dO, dweights, stream));
   ETR_TRY(expert_ffn_bwd(c, &route, b->dO, b->Xp, b->G, b->U, b->H, W1g, W1u, W2, b->dG, b->dU, b->dXp, dW1g, dW1u, dW2, b->stats, b->ws,
                          false, stream));
@@ -575,6 +589,7 @@ etr_status etr_block_forward(const etr_config* c, const etr_norm_config* n, cons
   ETR_TRY(check_ptrs({X, Xo, R, W1g, W1u, W2}));
   if (!aligned16(w_pre) || !aligned16(w_post) || !aligned16(gate)) return ETR_ERR_ALIGN;
   ETR_TRY(check_workspace(c, b, true, false));
+  ETR_TRY(check_layer_buffers(c, b, false));
   ETR_TRY(etr_prenorm(n, X, w_pre, bb->N, bb->rstd_x, stream));
   ETR_TRY(etr_layer_forward(c, bb->N, R, W1g, W1u, W2, b, bb->Y, stream));
   return etr_join(n, X, bb->Y, w_post, gate, nullptr, Xo, nullptr, bb->rstd_y, nullptr, stream);
@@ -589,6 +604,7 @@ etr_status etr_block_backward(const etr_config* c, const etr_norm_config* n, con
   for (const void* p : {(const void*)w_pre, (const void*)w_post, (const void*)gate, (const void*)dw_pre, (const void*)dw_post, (const void*)dgate})
     if (!aligned16(p)) return ETR_ERR_ALIGN;
   ETR_TRY(check_workspace(c, b, false, true));
+  ETR_TRY(check_layer_buffers(c, b, true));
   ETR_TRY(etr_join_bwd(n, dXo, nullptr, bb->Y, nullptr, w_post, gate, nullptr, bb->rstd_y, nullptr, dX, bb->dY, dw_post, dgate, nullptr,
                        bb->ws, stream));
   ETR_TRY(etr_layer_backward(c, bb->N, R, W1g, W1u, W2, bb->dY, b, bb->dN, dR, dW1g, dW1u, dW2, stream));

@@ -299,6 +299,8 @@ etr_status affinity_backward(const etr_config* c, const void* X, const float* R,
                              const etr_route* rt, const float* dgate, const float* ddelta,
                              const void* dXp_fused, void* dX, float* dR, void* ws, etr_stats* stats,
                              cudaStream_t st);
+// a plan's configuration and addresses (sort.cu)
+etr_status sort_check_plan(const etr_sort_config* c, const etr_sort_plan* p);
 // softmax-gate variant and load statistics (gate.cu)
 etr_status gate_softmax_forward(const etr_config* c, const float* delta, const etr_route* rt, float* lse,
                                 cudaStream_t st);

@@ -491,6 +491,11 @@ static etr_status sort_plan_ptrs(const etr_sort_config* c, const etr_sort_plan* 
   return ETR_OK;
 }
 
+etr_status sort_check_plan(const etr_sort_config* c, const etr_sort_plan* p) {
+  ETR_TRY(sort_valid(c));
+  return sort_plan_ptrs(c, p, {});
+}
+
 // Clusters of more than 8 CTAs are allowed per kernel and device.
 template <class K>
 static bool ensure_wide_cluster(K kernel, std::atomic<unsigned long long>& done) {

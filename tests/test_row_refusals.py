@@ -1,8 +1,12 @@
-"""Calls of the row operators that the Python binding refuses before it reaches the library, without a GPU."""
+"""Calls of the row operators that are refused before a launch: by the Python binding, and by the library for members of its structs.
+There is no GPU here: a launch, or a copy, would fail with another status."""
+import ctypes as C
+
 import pytest
 import torch
 
 from paper_2406_00023_b200 import etr
+from tests.test_rows_reference import composed
 
 
 def sort_calls(cfg, plan):
@@ -103,3 +107,40 @@ def test_composed_calls_check_the_configuration_first():
     for bad, code in ((dict(k=5), etr.ERR_SHAPE), (dict(h=0), etr.ERR_ARG), (dict(D=0), etr.ERR_ARG)):
         for name, call in composed_calls(buf, plan, bb).items():
             refused(lambda: call(etr.make_config(**dict(LAYER, **bad)), n), code, name)
+
+
+ROUTE = ("topk_idx", "counts", "slot_token", "gate", "tok_ptr", "tok_row")
+FORWARD = ("G", "U", "H", "O", "ws")
+BACKWARD = ("dO", "dG", "dU", "dXp")
+
+
+def changed(struct, name, value):
+    s = type(struct).from_buffer_copy(struct)
+    setattr(s.route if isinstance(s, etr.Buffers) and name in ROUTE else s, name, value)
+    return C.byref(s)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(gate_mode=etr.GATE_SOFTMAX), dict(fuse_dispatch=etr.FUSE_ON), dict(weight_dtype=etr.F32),
+                                dict(k=1), dict(dtype=etr.F32)], ids=str)
+def test_composed_calls_check_every_member_before_anything_runs(kw):
+    """A block's call launches the norm before the layer looks at its buffers, and the routed call clears the stats before the
+    plan is looked at: both have to know first."""
+    cfg = etr.make_config(**dict(dict(T=64, d=256, D=8, E=8, k=2, h=128, capacity=64, dtype=etr.BF16), **kw))
+    names, call, buf = composed(cfg, etr.make_norm_config(T=64, d=256, dtype=cfg.dtype, post_norm=True))
+    ok, soft, tensor_cores = 1 << 20, cfg.gate_mode == etr.GATE_SOFTMAX, cfg.dtype == etr.BF16
+    xp = () if cfg.fuse_dispatch == etr.FUSE_ON else ("Xp",)
+    affinity = ("delta", "xnorm", "rnorm") + (("lse",) if soft else ())
+    need = {"etr_routed_forward": FORWARD + ("Xp", "stats"), "etr_routed_backward": FORWARD + BACKWARD + ("Xp", "stats"),
+            "etr_block_forward": FORWARD + xp + affinity + ROUTE + ("stats",),
+            "etr_block_backward": FORWARD + BACKWARD + xp + affinity + ROUTE + ("dgate",) + (("ddelta",) if soft else ()) +
+            (("stats",) if tensor_cores else ())}
+    for name in names:
+        for x in need[name]:
+            for value, code in ((None, etr.ERR_ARG), (ok + 4, etr.ERR_ALIGN)):
+                assert call(name, buf=changed(buf, x, value)) == code, (name, x)
+        if "routed" in name:
+            for x, _ in etr.SortPlan._fields_:
+                for value, code in ((None, etr.ERR_ARG), (ok + 4, etr.ERR_ALIGN)):
+                    assert call(name, plan=changed(etr.SortPlan(*[ok] * 6), x, value)) == code, (name, x)
+    assert call("etr_block_forward", buf=changed(buf, "Z", ok + 4)) == etr.ERR_ALIGN
+    assert call("etr_block_backward", buf=changed(buf, "Z", None)) == etr.ERR_ARG
