@@ -244,7 +244,12 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     }
     if (device < 0) return Py_BuildValue("(is)", ETR_ERR_ARG, op.name);
     if (device != c10::cuda::current_device()) return Py_BuildValue("(is)", ETR_ERR_ARG, "tensors on another than the current device");
-    const etr_status code = call(g_fn[i], op.n, cfg, a, c10::cuda::getCurrentCUDAStream(device).stream());
+    void* const stream = c10::cuda::getCurrentCUDAStream(device).stream();
+    etr_status code;
+    // Other Python threads run meanwhile, as they do under ctypes: a launch can wait for a full queue or for a module to load.
+    Py_BEGIN_ALLOW_THREADS
+    code = call(g_fn[i], op.n, cfg, a, stream);
+    Py_END_ALLOW_THREADS
     return code == ETR_OK ? PyLong_FromLong(0) : Py_BuildValue("(is)", code, op.name);
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
