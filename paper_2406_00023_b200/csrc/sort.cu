@@ -496,6 +496,8 @@ etr_status sort_check_plan(const etr_sort_config* c, const etr_sort_plan* p) {
   return sort_plan_ptrs(c, p, {});
 }
 
+constexpr size_t SORT_SMEM = (size_t)(SORT_WARPS + SORT_ALONE + 3) * ETR_SORT_MAX_E * 4;        // of sort_plan_kernel, at most
+
 // Clusters of more than 8 CTAs are allowed per kernel and device.
 template <class K>
 static bool ensure_wide_cluster(K kernel, std::atomic<unsigned long long>& done) {
@@ -513,23 +515,54 @@ static int sort_pad_blocks(const etr_sort_config* c) { return c->align > 1 ? pad
 // One cluster of as many CTAs as have SORT_RUN pairs a warp, up to 16 of 16 warps (an opt-in size); longer batches take up to
 // 18 clusters of 8, and a launch before that counts the clusters' pairs.  Measured, a plan by itself: 32768 pairs of 32
 // experts 5.6 us in one cluster of 16 (7.6 of 8, 9.5 with the count, before those counts were written instead of read); 65536 of
-// 128 8.9 in one; 131072 of 64 9.4 with the count (14 without), 524288 16.
+// 128 8.9 in one; 131072 of 64 9.4 with the count (14 without), 524288 16.  widest: CTAs of the widest cluster that the device
+// takes; where that is less than a long batch's clusters have, one cluster takes any batch.
+struct PlanSplit { int warps, ncta, nclusters; };
+static PlanSplit plan_split(int pairs, int E, int widest) {
+  const int cta = SORT_WARPS * SORT_RUN;
+  if (pairs <= cta) {
+    const int warps = std::max(std::max((pairs + 31) / 32, (E + 63) / 64), 4);
+    return {std::min(warps, SORT_WARPS), 1, 1};
+  }
+  if (pairs > SORT_ONE_CLUSTER && widest >= SORT_CLUSTER)
+    return {SORT_WARPS, SORT_CLUSTER, std::min(pairs / (cta * SORT_CLUSTER) + 1, SORT_MAX_CLUSTERS)};
+  int ncta = 1;
+  while (ncta < widest && pairs > ncta * cta) ncta *= 2;
+  return {SORT_WARPS, ncta, 1};
+}
+
+// The widest cluster of the plan's kernel that the current device takes with the most shared memory that it can ask for, asked
+// once per device: 16 CTAs on a whole B200, but a process may have been given fewer SMs of each GPC.
+static int plan_widest() {
+  static std::atomic<int> cache[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SORT_ALONE;
+  int n = cache[dev & 63].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  for (n = SORT_ALONE; n > 1; n /= 2) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = n; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = n;
+    cfg.blockDim = SORT_WARPS * 32;
+    cfg.dynamicSmemBytes = SORT_SMEM;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, sort_plan_kernel, &cfg) == cudaSuccess && clusters > 0) break;
+    cudaGetLastError();
+  }
+  cache[dev & 63].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 static etr_status plan_launch(const etr_sort_config* c, const int32_t* ids, const etr_sort_plan* p, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0}, wide{0};
-  if (!ensure_dyn_smem(sort_plan_kernel, (size_t)(SORT_WARPS + SORT_ALONE + 3) * ETR_SORT_MAX_E * 4, done)) return ETR_ERR_CUDA;
+  if (!ensure_dyn_smem(sort_plan_kernel, SORT_SMEM, done)) return ETR_ERR_CUDA;
   if (!ensure_wide_cluster(sort_plan_kernel, wide)) return ETR_ERR_CUDA;
   SortShape s{c->T * c->k, c->k, c->E, c->align, c->capacity, sort_stride(c), (int)sort_rows_bound(c), 0};
-  const int cta = SORT_WARPS * SORT_RUN;
-  int warps = SORT_WARPS, ncta = 1, nclusters = 1;
-  if (s.N <= cta) {
-    warps = std::max(std::max(ceil_div(s.N, 32), ceil_div(s.E, 64)), 4);
-    warps = std::min(warps, SORT_WARPS);
-  } else if (s.N <= SORT_ONE_CLUSTER) {
-    while (ncta < SORT_ALONE && s.N > ncta * cta) ncta *= 2;
-  } else {
-    ncta = SORT_CLUSTER;
-    nclusters = std::min(s.N / (cta * SORT_CLUSTER) + 1, SORT_MAX_CLUSTERS);
-  }
+  const auto [warps, ncta, nclusters] = plan_split(s.N, s.E, plan_widest());
   const int all = warps * ncta * nclusters;
   s.run = ((s.N + all - 1) / all + 31) & ~31;
   if (nclusters > 1) {

@@ -86,3 +86,41 @@ def test_rows_without_a_token_are_filled_and_no_others(fill, ctas, warps, align,
     assert rows == sum(b - a for a, b in gaps) and total == sum((a + b - 1) * (b - a) // 2 for a, b in gaps)
     if gaps:
         assert (lowest, highest) == (gaps[0][0], gaps[-1][1] - 1)
+
+
+SPLIT = """
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+%s
+%s
+int main(int, char** a) {
+  const PlanSplit p = plan_split(atoi(a[1]), atoi(a[2]), atoi(a[3]));
+  printf("%%d %%d %%d", p.warps, p.ncta, p.nclusters);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def split(tmp_path_factory):
+    src = source()
+    rule = src[src.index("struct PlanSplit"):src.index("// The widest cluster of the plan's kernel")]
+    return compiled(SPLIT % ("\n".join(re.findall(r"constexpr int SORT_.*", src)), rule), tmp_path_factory.mktemp("split"))
+
+
+@pytest.mark.parametrize("widest", [1, 2, 4, 8, 16])
+def test_the_plan_keeps_to_the_clusters_that_a_device_takes(split, widest):
+    """No cluster wider than the device takes, whatever the batch; threads enough for two experts each; on a whole GPU one cluster
+    up to 65536 pairs and up to 18 of 8 CTAs above."""
+    for pairs in (0, 1, 512, 513, 1024, 1025, 4096, 4097, 8193, 65536, 65537, 200000, 600000, TOP):
+        for E in (1, 64, 257, 1024):
+            r = split(pairs, E, widest)
+            assert r.returncode == 0, r.stderr
+            warps, ncta, nclusters = map(int, r.stdout.split())
+            assert 1 <= ncta <= widest and 4 <= warps <= 16 and 64 * warps >= E and 1 <= nclusters <= 18
+            assert ncta == 8 or nclusters == 1
+            assert (nclusters > 1) == (pairs > 65536 and widest >= 8)
+            if ncta > 1 or pairs > 512:
+                assert warps == 16
+            if widest == 16 and pairs <= 65536:
+                assert ncta == min(16, max(1, 1 << max(0, (pairs - 1) // 512).bit_length()))
