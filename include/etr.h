@@ -489,7 +489,11 @@ etr_status etr_routed_backward(const etr_config* cfg, const float* weights, cons
 
 /* Rows of d values (d % 8 == 0, d <= ETR_NORM_MAX_D) of `dtype`; gains, gates, 1/rms and their gradients fp32; pointers 16-byte
  * aligned.  r(x) = 1 / sqrt(mean x^2 + eps), eps > 0.  A NULL gain or gate means ones.  T = 0 writes zero weight gradients
- * and nothing else.  Values and gradients below 1e17 in size (their squares and products are summed in fp32).
+ * and nothing else.
+ * Sizes: squares and products of a row's values are summed in fp32, so each of these has to stay below 1e17: X of etr_prenorm, Y, and
+ * etr_join's sum a X + b gate w_post (..) before it is rounded (beyond that the squares overflow: 1/rms is 0, and N a row of
+ * zeros); in the backward calls g = w dN or w_next dN, the sum's whole gradient G = dXo + rstd_o (g - xh <g, xh> / d) and
+ * w_post G, and g and w_post G also times 1/rms of their row of X, Xo or Y, which is up to 1 / sqrt(eps).
  * Xo may be X, and dX may be dXo or dres (the residual stream updated in place); no other output may overlap an input. */
 #define ETR_NORM_MAX_D 16384
 typedef struct etr_norm_config {
