@@ -430,7 +430,7 @@ class SortBuffers:
         base = (self.block.data_ptr() + 255) // 256 * 256
         self.device = self.block.get_device()          # -1: not on a GPU, which every call refuses
         both = SortPlanFor(made=cfg, device=self.device)               # a copy of cfg
-        self.c, self.cfg = both.plan, both.made
+        self.c, self.cfg = both.plan, SortConfig.from_buffer_copy(cfg)
         _check(lib().etr_sort_plan_bind(C.byref(cfg), C.c_void_p(base), n, C.byref(self.c), None), "etr_sort_plan_bind")
         for name, shape in (("counts", (cfg.E,)), ("offsets", (cfg.E + 1,)), ("totals", (4,)), ("row_token", (self.n_rows,)),
                             ("pos", (cfg.T, cfg.k))):

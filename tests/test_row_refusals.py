@@ -43,6 +43,16 @@ def test_a_plan_of_another_configuration_is_refused_for_that(other):
         refused(lambda: call(cfg), etr.ERR_WORKSPACE, name, "plan: made for another configuration")
 
 
+def test_a_plan_keeps_the_configuration_that_it_was_made_for():
+    """Whatever becomes of the two configurations that a caller can reach, its own and the plan's."""
+    cfg = etr.make_sort_config(T=4, k=2, E=3, d=16, dtype=etr.BF16)
+    plan = etr.SortBuffers(cfg, device="cpu")
+    assert bytes(plan.cfg) == bytes(cfg)
+    cfg.T = plan.cfg.T = 5
+    for name, call in sort_calls(cfg, plan).items():
+        refused(lambda: call(plan.cfg), etr.ERR_WORKSPACE, name, "plan: made for another configuration")
+
+
 # ---- the composed calls ------------------------------------------------------------------------------
 LAYER = dict(T=4, d=64, D=8, E=4, k=2, h=64, capacity=4, dtype=etr.BF16)
 
