@@ -169,6 +169,12 @@ at::ScalarType type_of(Kind kind, const Sizes& z) {
   }
 }
 
+// Other Python threads run during a call, as they do under ctypes: a launch can wait for a full queue or for a module to load.
+struct Unlocked {
+  PyThreadState* const state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // run(op, config address, arguments...): 0, or (status, what was wrong).  Handles are addresses of PlanFor, LayerFor, BlockFor and of a
 // norm's configuration; they are looked over before the tensors, since the kernels write through their addresses.  Nothing
 // here allocates or waits.
@@ -246,10 +252,10 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (device != c10::cuda::current_device()) return Py_BuildValue("(is)", ETR_ERR_ARG, "tensors on another than the current device");
     void* const stream = c10::cuda::getCurrentCUDAStream(device).stream();
     etr_status code;
-    // Other Python threads run meanwhile, as they do under ctypes: a launch can wait for a full queue or for a module to load.
-    Py_BEGIN_ALLOW_THREADS
-    code = call(g_fn[i], op.n, cfg, a, stream);
-    Py_END_ALLOW_THREADS
+    {
+      const Unlocked meanwhile;
+      code = call(g_fn[i], op.n, cfg, a, stream);
+    }
     return code == ETR_OK ? PyLong_FromLong(0) : Py_BuildValue("(is)", code, op.name);
   } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());

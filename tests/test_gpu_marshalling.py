@@ -11,28 +11,44 @@ from paper_2406_00023_b200 import etr
 
 pytestmark = pytest.mark.gpu
 
-SLOW = """
+FAKES = """
 #include <time.h>
-int slow(const void* cfg, void* X, void* w, void* N, void* rstd, void* stream) {
+#include <stdexcept>
+extern "C" int slow(const void* cfg, void* X, void* w, void* N, void* rstd, void* stream) {
   struct timespec t = {0, 500000000};
   nanosleep(&t, 0);
   return 0;
 }
+extern "C" int throws(const void* cfg, void* X, void* w, void* N, void* rstd, void* stream) { throw std::runtime_error("no memory for a record"); }
 """
+EXTRA = ("etr_sort_n_rows", "etr_norm_workspace_bytes", "etr_validate")
 
 
-def test_other_threads_run_during_a_call(tmp_path):
-    """A function of half a second in the place of etr_prenorm: a thread that wakes every 5 ms goes on meanwhile."""
-    src, so = tmp_path / "slow.c", tmp_path / "slow.so"
-    src.write_text(SLOW)
-    subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(so), str(src)])
-    slow = C.cast(C.CDLL(str(so)).slow, C.c_void_p).value
-    cfg = etr.make_norm_config(T=4, d=64, dtype=etr.BF16)
+@pytest.fixture
+def prenorm_by(tmp_path):
+    """Binds a function of FAKES in the place of etr_prenorm, which is put back afterwards."""
+    src, so = tmp_path / "fakes.cpp", tmp_path / "fakes.so"
+    src.write_text(FAKES)
+    subprocess.check_call(["g++", "-shared", "-fPIC", "-o", str(so), str(src)])
+    fakes = C.CDLL(str(so))
     X, N = (torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cfg = etr.make_norm_config(T=4, d=64, dtype=etr.BF16)
     etr.prenorm(cfg, X, None, N)                           # binds the library's functions
     from paper_2406_00023_b200 import _args
-    extra = ("etr_sort_n_rows", "etr_norm_workspace_bytes", "etr_validate")
-    real = [C.cast(getattr(etr.lib(), n), C.c_void_p).value for n in _args.names + extra]
+    real = {n: C.cast(getattr(etr.lib(), n), C.c_void_p).value for n in _args.names + EXTRA}
+
+    def bind(name):
+        _args.bind(*dict(real, etr_prenorm=C.cast(getattr(fakes, name), C.c_void_p).value).values())
+        return lambda: etr.prenorm(cfg, X, None, N)
+
+    yield bind
+    _args.bind(*real.values())
+    etr.prenorm(cfg, X, None, N)
+    torch.cuda.synchronize()
+
+
+def test_other_threads_run_during_a_call(prenorm_by):
+    """A function of half a second: a thread that wakes every 5 ms goes on meanwhile."""
     woken, stop = [], threading.Event()
 
     def tick():
@@ -40,19 +56,22 @@ def test_other_threads_run_during_a_call(tmp_path):
             woken.append(time.monotonic())
             time.sleep(0.005)
 
-    thread = threading.Thread(target=tick)
+    call, thread = prenorm_by("slow"), threading.Thread(target=tick)
     thread.start()
     try:
-        _args.bind(*[slow if n == "etr_prenorm" else a for n, a in zip(_args.names + extra, real)])
         beg = time.monotonic()
-        etr.prenorm(cfg, X, None, N)
+        call()
         end = time.monotonic()
     finally:
-        _args.bind(*real)
         stop.set()
         thread.join()
     assert end - beg >= 0.5
-    # a hundred times if nothing else runs; the thread that holds the lock lets it wake twice at most, before and after
+    # a hundred times if nothing else runs; where the call keeps the lock, never
     assert sum(beg + 0.05 < t < end - 0.05 for t in woken) >= 10
-    etr.prenorm(cfg, X, None, N)
-    torch.cuda.synchronize()
+
+
+def test_an_exception_of_the_library_is_a_python_one(prenorm_by):
+    call = prenorm_by("throws")
+    for _ in range(2):
+        with pytest.raises(RuntimeError, match="no memory for a record"):
+            call()
