@@ -121,7 +121,8 @@ __device__ __forceinline__ void load_gain(const float* w, int col, float2* out) 
 // itself, so that a wait for its own copies is all the synchronisation the ring needs.  Pieces behind a row's end and rows
 // behind the last arrive as zeros (a copy of no bytes).  A second tile ahead cost time (bf16: prenorm of 65536 x 4096 167 us
 // with one, 188 with two; join backward of 16384 x 4096 137 and 145).  RING false: rows so long that two tiles do not
-// fit shared memory come straight from global memory.
+// fit shared memory come straight from global memory (join backward from d > 12288 in bf16 and d > 6144 in fp32 on, prenorm backward
+// from d > 8192 and join from d > 12288 on, both in fp32).
 template <int NT, int NV, bool RING>
 struct RowRing {
   uint32_t smem;                                  // this thread's first slot
@@ -148,7 +149,11 @@ struct RowRing {
 // and 1024 with 64 for a prenorm whose block is more than 384 threads, so that two fit (fp32 40920 x 3280: 72 % of the copy
 // rate with one, 97 with two; smaller blocks lose: 20000 x 1088 bf16 75 and 67 %); prenorm's backward 576 with 112, which fits a
 // third block of 192 threads (20000 x 1088: 49 % with two, 76 with three); the join's backward, and rows of more than 2
-// pieces a thread, 512 with 128 (the join's spills at 112).
+// pieces a thread, 512 with 128 (the join's spills at 112).  128 registers do not hold the gains and their gradients of every row of more
+// than 2 pieces: the join's backward spills 304 to 312 bytes a thread in bf16 (d > 8192) and 428 in fp32 (d > 8192), prenorm's
+// 24 in bf16.  Of the copy rate, at 2^27 values: join backward bf16 d = 8192 95 %, 10240 to 16384 37 to 54; fp32 6144 93, 8192 (no
+// ring) 66, 12288 to 16384 41 to 46; prenorm backward bf16 8192 100, above 70 to 84; fp32 8192 99, above (no ring) 49 to 58;
+// join fp32 12288 92, above (no ring) 54 to 63; all other forward forms 83 to 100.
 constexpr int norm_bwd_threads(bool join, int nv) { return join || nv > 2 ? 512 : 576; }
 
 // Forward.  JOIN false: prenorm of X.  Blocks walk tiles of rpb rows in strides, with the gains in registers.  HBM-bound: bf16, prenorm of
@@ -249,7 +254,7 @@ norm_fwd_kernel(const NormArgs p, const RowShape sh) {
   }
 }
 
-// Backward, HBM-bound: bf16, join of 65536 x 4096 491 us (the copy rate), prenorm of 16384 x 2048 45 us (90 %, 3 us of them
+// Backward, HBM-bound: bf16, join of 65536 x 4096 486 to 531 us from box to box (92 to 100 %), prenorm of 16384 x 2048 45 us (90 %, 3 us of them
 // norm_dw_kernel).  Blocks walk tiles of rpb rows in strides, a thread always on the same columns, so the gains' gradients add up in
 // registers; a block leaves one row of partial sums per gain, which norm_dw_kernel adds in order.
 // JOIN false: prenorm (Xo_in is its input X, dXo the gradient that comes along the residual, may be NULL; no y).

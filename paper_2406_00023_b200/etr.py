@@ -442,8 +442,8 @@ class SortBuffers:
 
 
 # The row operators and the calls composed of them go through csrc/args.cpp, which looks every tensor and buffer over (type, place,
-# order, size: refusals are EtrError) and calls the C function on the current stream: 0.5 to 1 us a call instead of 5 to 10
-# through ctypes.
+# order, size: refusals are EtrError) and calls the C function on the current stream: 0.3 us a call besides the launch,
+# instead of 5 to 10 through ctypes.
 _ROW_OPS = ("etr_sort", "etr_sort_rows", "etr_sort_rows_bwd", "etr_unsort_rows", "etr_unsort_rows_bwd", "etr_prenorm", "etr_prenorm_bwd",
             "etr_join", "etr_join_bwd", "etr_routed_forward", "etr_routed_backward", "etr_block_forward", "etr_block_backward")
 
