@@ -103,3 +103,32 @@ def test_rows_across_clusters():
         etr.sort_rows_bwd(cfg, Xs, buf, dX)
         rr.assert_within(Y, *rr.unsort(Xs, w, buf.pos, X.dtype), "Y")
         rr.assert_within(dX, *rr.unsort(Xs, None, buf.pos, X.dtype), "dX")
+
+
+@pytest.mark.parametrize("lost", [0, 300])
+def test_the_most_pairs_that_a_plan_takes(lost):
+    """2^31 - 65537 pairs, pair i of expert i mod 7, the last `lost` without an expert: the rows are known without a sort.  Behind the
+    last row nothing, or 300 rows without a token, are left to fill."""
+    n, E, step = 2 ** 31 - 65537, 7, 1 << 28
+    cfg = etr.make_sort_config(T=n, k=1, E=E, d=8, dtype=etr.BF16)
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("60 GB of device memory")
+    buf = etr.SortBuffers(cfg)
+    ids = torch.empty(n, 1, dtype=torch.int32, device="cuda")
+    for i in range(0, n, step):
+        ids[i:i + step, 0] = torch.arange(i, min(i + step, n), device="cuda") % E
+    ids[n - lost:] = -1
+    etr.sort(cfg, ids, buf)
+    del ids
+    kept = n - lost
+    counts = torch.tensor([(kept + E - 1 - e) // E for e in range(E)])
+    offsets = torch.cat([torch.zeros(1, dtype=torch.long), counts.cumsum(0)])
+    assert buf.counts.tolist() == counts.tolist() and buf.offsets.tolist() == offsets.tolist() and buf.totals.tolist() == [kept, 0, lost, 0]
+    start = offsets.cuda()
+    for i in range(0, n, step):
+        at = torch.arange(i, min(i + step, n), device="cuda")
+        row = torch.where(at < kept, start[at % E] + at // E, -1)
+        assert torch.equal(buf.pos[i:i + step, 0].long(), row)
+        has = row >= 0
+        assert torch.equal(buf.row_token[row[has]].long(), at[has])
+    assert bool((buf.row_token[kept:] == -1).all())

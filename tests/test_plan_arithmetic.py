@@ -1,4 +1,4 @@
-"""Index arithmetic of the plan of a given choice at sizes that no test can allocate: pieces of the kernel's and the launch's source,
+"""Index arithmetic of the plan of a given choice up to its largest sizes: pieces of the kernel's and the launch's source,
 compiled for the host with checks of signed overflow."""
 import os
 import re
