@@ -31,14 +31,15 @@ struct LayerFor {
   etr_buffers buf;
   etr_config made;
   int32_t device;
-  // Buffers of a larger layer serve a smaller one.  The scratch has a size of its own, which the C call checks.
-  bool fits(const etr_config& c) const {
+  // Buffers of a larger layer serve a smaller one.  The scratch has a size of its own, which the C call checks.  router: the layer's
+  // own router runs too, whose members are as long as the batch; the experts alone need the rows.
+  bool fits(const etr_config& c, bool router) const {
     const auto rows = [](const etr_config& q) { return (int64_t)q.E * ((q.capacity + 127ll) / 128 * 128); };
     const auto bytes = [](const etr_config& q) { return q.dtype == ETR_BF16 ? 2 : 4; };
     const __int128 has = rows(made) * bytes(made), wants = rows(c) * bytes(c);
-    return wants * c.d <= has * made.d && wants * c.h <= has * made.h && rows(c) <= rows(made) && c.T <= made.T && c.E <= made.E &&
-           (int64_t)c.T * c.k <= (int64_t)made.T * made.k && (int64_t)c.T * c.E <= (int64_t)made.T * made.E &&
-           (int64_t)c.T * (c.d / c.D) <= (int64_t)made.T * (made.d / made.D);
+    if (wants * c.d > has * made.d || wants * c.h > has * made.h) return false;
+    return !router || (rows(c) <= rows(made) && c.T <= made.T && c.E <= made.E && (int64_t)c.T * c.k <= (int64_t)made.T * made.k &&
+                       (int64_t)c.T * c.E <= (int64_t)made.T * made.E && (int64_t)c.T * (c.d / c.D) <= (int64_t)made.T * (made.d / made.D));
   }
 };
 struct BlockFor {
@@ -206,7 +207,7 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         fits = static_cast<PlanFor*>(p)->fits(z.sort);
         on[j] = static_cast<PlanFor*>(p)->device;
       } else if (w.kind == LAYER_BUF) {
-        fits = static_cast<LayerFor*>(p)->fits(*static_cast<const etr_config*>(cfg));
+        fits = static_cast<LayerFor*>(p)->fits(*static_cast<const etr_config*>(cfg), op.arg[0].kind == NORM_CFG);
         on[j] = static_cast<LayerFor*>(p)->device;
       } else if (w.kind == BLOCK_BUF) {
         fits = static_cast<BlockFor*>(p)->fits(*static_cast<const etr_norm_config*>(a[0]));

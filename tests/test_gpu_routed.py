@@ -106,3 +106,21 @@ def test_buffers_of_a_larger_layer_serve_a_smaller_one():
         torch.cuda.synchronize()
         out.append([a[x].clone() for x in ("Y", "Xo", "dX", "dweights", "dW1g", "dW2", "dR", "dw_pre")])
     assert all(torch.equal(p, q) for p, q in zip(*out))
+
+
+def test_routed_calls_use_nothing_of_the_layers_own_router():
+    """Buffers whose members of the batch's length are too short for the layer's own call, but whose rows suffice."""
+    a, names = everything()
+    short = etr.LayerBuffers(etr.make_config(T=8, d=256, D=32, E=8, k=1, h=64, capacity=48, dtype=etr.BF16))
+    short.block.fill_(0x5a)
+    out = []
+    for buf in (a["buf"], short):
+        for name in ("routed_forward", "routed_backward"):
+            getattr(etr, name)(*[buf if x == "buf" else a[x] for x in names[name]])
+        torch.cuda.synchronize()
+        out.append([a[x].clone() for x in ("Y", "dX", "dweights", "dW1g", "dW1u", "dW2")])
+    assert all(torch.equal(p, q) for p, q in zip(*out))
+    for name in ("block_forward", "block_backward"):
+        with pytest.raises(etr.EtrError) as e:
+            getattr(etr, name)(*[short if x == "buf" else a[x] for x in names[name]])
+        assert e.value.code == etr.ERR_WORKSPACE

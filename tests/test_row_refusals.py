@@ -89,15 +89,17 @@ def test_composed_calls_refuse_a_plan_of_another_configuration(other):
             refused(lambda: call(cfg, n), etr.ERR_WORKSPACE, name, "plan: made for another configuration")
 
 
-@pytest.mark.parametrize("other, fits", [
-    (dict(T=3), False), (dict(E=3), False), (dict(d=32, D=4), False), (dict(h=32), False), (dict(k=1), False), (dict(capacity=0x80, E=3), False),
-    (dict(dtype=etr.BF16, h=8), False), (dict(T=5, E=5, k=3, d=128, h=128, capacity=300), True), (dict(dtype=etr.F32), True), (dict(), True)], ids=str)
-def test_composed_calls_refuse_buffers_of_a_smaller_layer(other, fits):
+@pytest.mark.parametrize("other, experts, router", [
+    # members as long as the batch: the layer's own router's alone
+    (dict(T=3), True, False), (dict(k=1), True, False), (dict(D=16), True, False), (dict(E=2, capacity=200), True, False),
+    (dict(E=3), False, False), (dict(d=32, D=4), False, False), (dict(h=32), False, False), (dict(capacity=0x80, E=3), False, False),
+    (dict(T=5, E=5, k=3, d=128, h=128, capacity=300), True, True), (dict(dtype=etr.F32), True, True), (dict(), True, True)], ids=str)
+def test_composed_calls_refuse_buffers_of_a_smaller_layer(other, experts, router):
     """Buffers of a larger one serve as they do for the layer's own calls: what is wrong then is that these are not on a GPU."""
     small = etr.LayerBuffers(etr.make_config(**dict(LAYER, gemm_impl=etr.GEMM_SIMT, **other)), device="cpu")
     cfg, n, _, plan, bb = made()
     for name, call in composed_calls(small, plan, bb).items():
-        if fits:
+        if router if "block" in name else experts:
             refused(lambda: call(cfg, n), etr.ERR_ARG, name, "buf: not on a CUDA device")
         else:
             refused(lambda: call(cfg, n), etr.ERR_WORKSPACE, name, "buf: made for another configuration")
